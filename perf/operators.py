@@ -240,8 +240,9 @@ def _plain_weigh(s):
     lse[b, i] = s["lse"]
     lse = lse.view(*lse.shape[:2], c["kv_heads"], -1).permute(0, 2, 3, 1).reshape(len(s["new"]), c["kv_heads"], -1, 1)
     given = score.sub_(lse).exp_().sum(2)
-    live = (torch.arange(max(s["lens"]), device="cuda") < s["lens_dev"][:, None])[:, None]
-    s["weights"].copy_(torch.where(live, DECAY * s["weights"] + given, s["weights"]))
+    pos, n = torch.arange(max(s["lens"]), device="cuda"), s["lens_dev"][:, None]
+    old = torch.where((pos < n - s["new_dev"][:, None])[:, None], DECAY * s["weights"], torch.zeros_like(given))     # new rows begin with none
+    s["weights"].copy_(torch.where((pos < n)[:, None], old + given, s["weights"]))
     return s["weights"]
 
 
@@ -331,7 +332,9 @@ def exact(case, seed):
             x, _ = _exact_scores(s, b)
             first = sum(new[:b])
             p = torch.exp(x - s["lse"][first:first + new[b]].double().T[:, :, None])
-            w[b, :, :lens[b]] = DECAY * w[b, :, :lens[b]] + p.view(kv, group, new[b], -1).sum((1, 2))
+            w[b, :, :lens[b] - new[b]] *= DECAY
+            w[b, :, lens[b] - new[b]:lens[b]] = 0
+            w[b, :, :lens[b]] += p.view(kv, group, new[b], -1).sum((1, 2))
         return w
     k, v, w_out, kept = s["k_cache"].clone(), s["v_cache"].clone(), s["weights_out"].double(), s["kept"]
     table, budget = s["table"].cpu(), c["budget"]
