@@ -344,6 +344,80 @@ int32_t flover_k_gated_workspace_bytes(int32_t dtype, int32_t M, int32_t F, int3
 int32_t flover_k_gated_mlp(int32_t dtype, const void* x, const void* w_tiled, int32_t M, int32_t F, int32_t K,
                            int32_t context_pass, void* act, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ operators on a cache kept in pages
+ * A serving loop around the fused step: prompts arrive in chunks beside requests that decode, heads may share keys, caches
+ * lie in pages, attention may be bounded by a window, and a cache may be cut down to its heaviest rows.
+ * One layer's cache is kcache, vcache [device][n_pages][n_kv_head][page_size][head_dim]; position p of a sequence lies in row
+ * p % page_size of page table[p / page_size].  A slot cache [C][n_head][S][head_dim] is the case page_size = S with one page
+ * per sequence.  Query head h reads key head h / (n_head / n_kv_head). */
+typedef struct flover_paged_shape {
+  int32_t dtype;                         /* FLOVER_F32 | FLOVER_F16 | FLOVER_BF16: queries, cache, output */
+  int32_t n_head, n_kv_head, head_dim;   /* n_head a multiple of n_kv_head; head_dim in {64,128} */
+  int32_t page_size, n_pages;            /* page_size a multiple of 16, or any size if no sequence has a second page;
+                                            n_pages * n_kv_head * page_size < 2^31 */
+  int32_t window, sinks;                 /* window > 0: position p sees its last `window` positions, itself among them, and the first
+                                            `sinks`; window == 0: all up to itself (sinks is not read then) */
+} flover_paged_shape;
+
+/* What one iteration knows about its sequences, checked on the host and laid out in device memory once, for the calls of all
+ * layers.  new_len, len [host][n_seq]: 0 <= new_len[i] <= len[i], the sequence's new tokens and its cached rows with them; the
+ * new tokens are its last positions.  Sequences without rows or without new tokens are allowed anywhere in the list.
+ * table [host][n_seq][table_stride]: page numbers, of which the first ceil(len[i] / page_size) are read.  New tokens of all
+ * sequences lie one after the other in the calls' rows; T = sum of new_len.
+ * flover_k_paged_plan_bytes [host only] makes every check and returns the [device] memory that flover_k_paged_plan_set needs,
+ * for the lists and for the partial results of keys shared out to several blocks.
+ * flover_k_paged_plan_create takes the shape; flover_k_paged_plan_set lays a plan out in `memory` (256-byte aligned, the
+ * caller's, to stay until the last call that uses it is done) and enqueues the copy on `stream`; the lists are consumed before
+ * return, and it may be called again for the next iteration: the new lists are ordered on `stream` behind what is there.  Calls with
+ * the plan on another stream wait for that copy by themselves (not while they are captured into a graph: then the copy has to
+ * be done).  set cannot be captured (STATE).
+ * Calls that use one plan share its memory: they may not overlap each other; plans in memory of their own may.
+ * A captured call keeps the plan's launch shapes; it may be replayed until the plan is set again or destroyed.
+ * Errors: INVAL (shape, lengths, a page out of range, alignment), NOMEM, STATE, HIP. */
+typedef struct flover_paged_plan flover_paged_plan;
+int32_t flover_k_paged_plan_bytes(const flover_paged_shape* shape, int32_t n_seq, const int32_t* new_len, const int32_t* len,
+                                  const int32_t* table, int32_t table_stride, uint64_t* out);
+int32_t flover_k_paged_plan_create(const flover_paged_shape* shape, flover_paged_plan** out);
+int32_t flover_k_paged_plan_set(flover_paged_plan* plan, int32_t n_seq, const int32_t* new_len, const int32_t* len,
+                                const int32_t* table, int32_t table_stride, void* memory, uint64_t memory_bytes, void* stream);
+int32_t flover_k_paged_plan_destroy(flover_paged_plan* plan);   /* waits for the plan's last copy; NULL is a no-op */
+
+/* Rows of the new tokens to their places: k, v [device][T] rows of [n_kv_head][head_dim], k_stride / v_stride elements apart
+ * (a multiple of 16 bytes; views into a packed q|k|v row are fine), 16-byte aligned.  Refused (INVAL) where two sequences of
+ * the plan share a page that new tokens go to. */
+int32_t flover_k_paged_append(const flover_paged_plan* plan, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                              void* kcache, void* vcache, void* stream);
+
+/* Attention of the new tokens over their sequences' cached rows (their own among them: append first): causal, within the
+ * window if there is one.  out[t][h] = sum_j softmax_j(q[t][h] . K[j] / sqrt(head_dim)) V[j], fp32 scores, softmax and
+ * accumulation, rounded to dtype.  Keys that a token does not see do not reach its result, whatever they hold.
+ * q [device][T] rows of [n_head][head_dim], q_stride elements apart, 16-byte aligned; out [device][T][n_head][head_dim], apart from
+ * q and the caches; lse [device][T][n_head] fp32 or NULL: natural log of the sum of the exponentials of the scaled scores.
+ * Several sequences may share pages.  How a token's keys are shared out depends on the whole plan, so its last bits may differ
+ * between plans; the same plan gives the same bits. */
+int32_t flover_k_paged_attention(const flover_paged_plan* plan, const void* q, int64_t q_stride, const void* kcache,
+                                 const void* vcache, void* out, float* lse, void* stream);
+
+/* Attention weights that the new tokens gave to every cached row, summed over them and over the heads that share the row:
+ * weights[i][g][p] = old + sum exp(q . K[p] / sqrt(head_dim) - lse) for p < len[i], old = decay * weights[i][g][p] for the rows that
+ * were there before, 0 for the new tokens' own (whatever the place held); the rest stays.  One buffer per layer, one call per plan.
+ * q, lse as flover_k_paged_attention had and left them; weights [device][n_seq][n_kv_head] rows of fp32, weight_stride >= the longest
+ * sequence apart.  A decay of 0 overwrites.  Sums are taken in a fixed order. */
+int32_t flover_k_paged_weights(const flover_paged_plan* plan, const void* q, int64_t q_stride, const void* kcache, const float* lse,
+                               float decay, float* weights, int64_t weight_stride, void* stream);
+
+/* Eviction from the cache: every sequence of more than `budget` cached rows keeps, for each key head by itself, its first
+ * `first`, its last `recent` and the heaviest of the rest (the lowest position on ties, NaN as the lightest), `budget` in all.
+ * The kept rows move to the front in order, within the sequence's own pages; rows behind them stay as they were.  The caller's next
+ * plan has min(len, budget) rows for the sequence, and its further pages are free.
+ * weights: as above.  weights_out [device][n_seq][n_kv_head] rows of out_stride >= min(budget, longest): the kept rows' weights (the rest
+ * stays); may be `weights` itself with the same stride, otherwise apart from it; NULL: not wanted.  kept [device][n_seq][n_kv_head][budget]:
+ * the positions that were kept, -1 behind the last.  Refused (INVAL) where sequences of the plan share a page, and where
+ * first + recent > budget. */
+int32_t flover_k_paged_evict(const flover_paged_plan* plan, void* kcache, void* vcache, const float* weights, int64_t weight_stride,
+                             int32_t budget, int32_t first, int32_t recent, float* weights_out, int64_t out_stride, int32_t* kept,
+                             void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,8 @@ EXPORTED_SYMBOLS = [
     "flover_k_decode_attention", "flover_k_compact_workspace_bytes", "flover_k_compact", "flover_k_gemm_tiled_bytes",
     "flover_k_gemm_workspace_bytes", "flover_k_gemm_retile", "flover_k_gemm", "flover_add_request_cached",
     "flover_k_copy_probe", "flover_k_decode_attention_noalloc", "flover_k_gated_retile", "flover_k_gated_workspace_bytes", "flover_k_gated_mlp",
+    "flover_k_paged_plan_bytes", "flover_k_paged_plan_create", "flover_k_paged_plan_set", "flover_k_paged_plan_destroy",
+    "flover_k_paged_append", "flover_k_paged_attention", "flover_k_paged_weights", "flover_k_paged_evict",
 ]
 
 WEIGHT_FIELDS = ["wte", "wpe", "ln1_g", "ln1_b", "wqkv", "bqkv", "wo", "bo", "ln2_g", "ln2_b", "w1", "b1", "wu", "w2",
@@ -55,6 +57,11 @@ class _ReorderOut(C.Structure):
     _fields_ = [("capacity", C.c_int32), ("n_evicted", C.c_int32), ("evicted_req_id", C.c_void_p),
                 ("mem_offset", C.c_int32), ("new_lo", C.c_int32), ("new_size", C.c_int32), ("min_cost", C.c_int32),
                 ("n_moves", C.c_int32), ("move_src", C.c_void_p), ("move_dst", C.c_void_p), ("bytes_moved", C.c_int64)]
+
+
+class _PagedShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in
+                ["dtype", "n_head", "n_kv_head", "head_dim", "page_size", "n_pages", "window", "sinks"]]
 
 
 _lib = None
@@ -112,6 +119,15 @@ def load_library():
     L.flover_k_gated_workspace_bytes.argtypes = [C.c_int32] * 4 + [C.POINTER(C.c_uint64)]
     L.flover_k_gated_mlp.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                      C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+    L.flover_k_paged_plan_bytes.argtypes = [C.POINTER(_PagedShape), C.c_int32] + [C.c_void_p] * 3 + [C.c_int32, C.POINTER(C.c_uint64)]
+    L.flover_k_paged_plan_create.argtypes = [C.POINTER(_PagedShape), C.POINTER(C.c_void_p)]
+    L.flover_k_paged_plan_set.argtypes = [C.c_void_p, C.c_int32] + [C.c_void_p] * 3 + [C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]
+    L.flover_k_paged_plan_destroy.argtypes = [C.c_void_p]
+    L.flover_k_paged_append.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 3
+    L.flover_k_paged_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_int64] + [C.c_void_p] * 5
+    L.flover_k_paged_weights.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64,
+                                         C.c_void_p]
+    L.flover_k_paged_evict.argtypes = [C.c_void_p] * 4 + [C.c_int64] + [C.c_int32] * 3 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
     _lib = L
     return L
 
@@ -461,3 +477,186 @@ def k_copy_probe(dst: torch.Tensor, src: torch.Tensor):
     assert dst.is_contiguous() and src.is_contiguous() and dst.numel() * dst.element_size() == src.numel() * src.element_size()
     _check(load_library().flover_k_copy_probe(dst.data_ptr(), src.data_ptr(), src.numel() * src.element_size(),
                                               _stream_ptr()))
+
+
+# ------------------------------------------------------------------ operators on a cache kept in pages
+
+class PagedPlan:
+    """What one iteration knows about its sequences, checked and laid out on the current device once, for the calls of all layers.
+
+    dtype, n_head, n_kv_head, head_dim, page_size, n_pages: the cache of one layer is a pair of tensors
+    [n_pages][n_kv_head][page_size][head_dim].  new_len, length: host ints [n_seq], the sequences' new tokens and their cached rows
+    with them.  table: host ints [n_seq][at least ceil(length / page_size)], or a list of lists of page numbers.  window, sinks: see
+    flover_paged_shape.  Calls that use one plan share its memory and may not overlap each other."""
+
+    def __init__(self, dtype: torch.dtype, n_head: int, n_kv_head: int, head_dim: int, page_size: int, n_pages: int, new_len, length,
+                 table, window: int = 0, sinks: int = 0):
+        self._handle = None
+        if dtype not in _DT_OF:
+            raise FloverError("dtype %s: float32, float16 or bfloat16" % dtype)
+        self.dtype, self.n_head, self.n_kv_head, self.head_dim, self.page_size, self.n_pages = \
+            dtype, n_head, n_kv_head, head_dim, page_size, n_pages
+        self._shape = _PagedShape(_DT_OF[dtype], n_head, n_kv_head, head_dim, page_size, n_pages, window, sinks)
+        self.memory, self.stream = None, None
+        lists = self._lists(new_len, length, table)
+        handle = C.c_void_p()
+        _check(load_library().flover_k_paged_plan_create(C.byref(self._shape), C.byref(handle)))
+        self._handle = handle
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self._cache_shape = (n_pages, n_kv_head, page_size, head_dim)
+        self._set(lists)
+
+    def _lists(self, new_len, length, table):
+        new_len, length = _i32(new_len), _i32(length)
+        if len(new_len) == 0:
+            table = np.zeros((0, 0), np.int32)
+        elif isinstance(table, (list, tuple)):
+            rows = [_i32(r).reshape(-1) for r in table]
+            table = np.full((len(rows), max(map(len, rows), default=0)), -1, np.int32)
+            for i, r in enumerate(rows):
+                table[i, :len(r)] = r
+        table = _i32(table)
+        if new_len.ndim != 1 or length.shape != new_len.shape or table.ndim != 2 or len(table) != len(new_len):
+            raise FloverError("new_len, length [n_seq] and table [n_seq][pages]")
+        n = C.c_uint64()
+        _check(load_library().flover_k_paged_plan_bytes(C.byref(self._shape), len(new_len), new_len.ctypes.data, length.ctypes.data,
+                                                        table.ctypes.data, table.shape[1], C.byref(n)))
+        return new_len, length, table, int(n.value)
+
+    def _set(self, lists):
+        new_len, length, table, need = lists
+        stream = torch.cuda.current_stream(self.device)
+        if self.memory is None or self.memory.numel() < need:
+            self.memory = torch.empty(need + need // 2, dtype=torch.uint8, device=self.device)     # the next iterations' lists fit too
+        elif stream.cuda_stream != self.stream:
+            self.memory.record_stream(stream)
+        with torch.cuda.device(self.device):
+            _check(load_library().flover_k_paged_plan_set(self._handle, len(new_len), new_len.ctypes.data, length.ctypes.data,
+                                                          table.ctypes.data, table.shape[1], self.memory.data_ptr(),
+                                                          self.memory.numel(), stream.cuda_stream))
+        self.stream = stream.cuda_stream
+        self.n_seq, self.tokens, self.longest = len(new_len), int(new_len.sum()), int(length.max()) if len(length) else 0
+
+    def update(self, new_len, length, table):
+        """The next iteration's lists, ordered on the current stream behind the calls that used the present ones there."""
+        self._set(self._lists(new_len, length, table))
+
+    def close(self):
+        if self._handle is not None:
+            load_library().flover_k_paged_plan_destroy(self._handle)
+            self._handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # ---- what the calls check of their tensors
+    def _on(self, *tensors):
+        """Stream of a call on these tensors."""
+        for t in tensors:
+            if t.device != self.device:
+                raise FloverError("tensor on %s, plan on %s" % (t.device, self.device))
+        stream = torch.cuda.current_stream(self.device)
+        if stream.cuda_stream != self.stream:
+            self.memory.record_stream(stream)
+        return stream.cuda_stream
+
+    def _cache(self, t: torch.Tensor, name: str) -> int:
+        if t.shape != self._cache_shape or t.dtype != self.dtype or not t.is_contiguous():
+            raise FloverError("%s: contiguous %s of %s" % (name, list(self._cache_shape), self.dtype))
+        return t.data_ptr()
+
+    def _rows(self, t: torch.Tensor, heads: int, name: str) -> torch.Tensor:
+        """t itself, or a copy where its rows are not whole or not on 16 bytes."""
+        if t.shape != (self.tokens, heads, self.head_dim) or t.dtype != self.dtype:
+            raise FloverError("%s: [%d][%d][%d] of %s" % (name, self.tokens, heads, self.head_dim, self.dtype))
+        row, head, one = t.stride()
+        if t.numel() and (one != 1 or (head != self.head_dim and heads > 1) or row < heads * self.head_dim or t.data_ptr() % 16 or
+                          row * t.element_size() % 16):
+            t = t.contiguous()
+            t = t if t.data_ptr() % 16 == 0 else t.clone()
+        return t
+
+    def _weights(self, t: torch.Tensor, least: int, name: str) -> int:
+        """Row stride of [n_seq][n_kv_head][>= least] fp32."""
+        if t.dtype != torch.float32 or t.dim() != 3 or t.shape[:2] != (self.n_seq, self.n_kv_head) or t.shape[2] < least:
+            raise FloverError("%s: float32 [%d][%d][at least %d]" % (name, self.n_seq, self.n_kv_head, least))
+        if t.numel() == 0:
+            return max(t.shape[2], 1)
+        row = t.stride(1) if self.n_kv_head > 1 else t.stride(0) if self.n_seq > 1 else t.shape[2]
+        if (t.stride(2) != 1 and t.shape[2] > 1) or row < t.shape[2] or (self.n_seq > 1 and t.stride(0) != self.n_kv_head * row):
+            raise FloverError("%s: rows of consecutive elements, one stride apart" % name)
+        return row
+
+    def _call(self, function, stream, *args):
+        if torch.cuda.current_device() == self.device.index:
+            _check(function(self._handle, *args, stream))
+        else:
+            with torch.cuda.device(self.device):
+                _check(function(self._handle, *args, stream))
+
+
+def k_paged_append(plan: PagedPlan, k: torch.Tensor, v: torch.Tensor, kcache: torch.Tensor, vcache: torch.Tensor):
+    """k, v [tokens][n_kv_head][head_dim] (views into packed rows are fine) to their places in the caches, which are returned."""
+    stream = plan._on(k, v, kcache, vcache)
+    kp, vp = plan._rows(k, plan.n_kv_head, "k"), plan._rows(v, plan.n_kv_head, "v")
+    width = plan.n_kv_head * plan.head_dim
+    plan._call(load_library().flover_k_paged_append, stream, kp.data_ptr(), max(kp.stride(0), width), vp.data_ptr(),
+               max(vp.stride(0), width), plan._cache(kcache, "kcache"), plan._cache(vcache, "vcache"))
+    return kcache, vcache
+
+
+def k_paged_attention(plan: PagedPlan, q: torch.Tensor, kcache: torch.Tensor, vcache: torch.Tensor,
+                      out: Optional[torch.Tensor] = None, lse=None):
+    """Attention of the new tokens q [tokens][n_head][head_dim] over their sequences' cached rows.  lse: fp32 [tokens][n_head], or
+    True to have it made; then (out, lse) is returned, otherwise out."""
+    qp = plan._rows(q, plan.n_head, "q")
+    if out is None:
+        out = torch.empty((plan.tokens, plan.n_head, plan.head_dim), dtype=plan.dtype, device=plan.device)
+    elif out.shape != qp.shape or out.dtype != plan.dtype or not out.is_contiguous():
+        raise FloverError("out: contiguous, as q")
+    if lse is True:
+        lse = torch.empty((plan.tokens, plan.n_head), dtype=torch.float32, device=plan.device)
+    elif lse is False:
+        lse = None
+    if lse is not None and (lse.shape != (plan.tokens, plan.n_head) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise FloverError("lse: contiguous float32 [%d][%d]" % (plan.tokens, plan.n_head))
+    stream = plan._on(q, kcache, vcache, out) if lse is None else plan._on(q, kcache, vcache, out, lse)
+    plan._call(load_library().flover_k_paged_attention, stream, qp.data_ptr(), max(qp.stride(0), plan.n_head * plan.head_dim),
+               plan._cache(kcache, "kcache"), plan._cache(vcache, "vcache"), out.data_ptr(), lse.data_ptr() if lse is not None else None)
+    return out if lse is None else (out, lse)
+
+
+def k_paged_weights(plan: PagedPlan, q: torch.Tensor, kcache: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor,
+                    decay: float = 1.0):
+    """weights [n_seq][n_kv_head][>= longest] fp32 = decay * weights (of the new tokens' own rows: 0) + the attention weights of
+    the new tokens, in place."""
+    qp = plan._rows(q, plan.n_head, "q")
+    if lse.shape != (plan.tokens, plan.n_head) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise FloverError("lse: contiguous float32 [%d][%d]" % (plan.tokens, plan.n_head))
+    stride = plan._weights(weights, plan.longest, "weights")
+    stream = plan._on(q, kcache, lse, weights)
+    plan._call(load_library().flover_k_paged_weights, stream, qp.data_ptr(), max(qp.stride(0), plan.n_head * plan.head_dim),
+               plan._cache(kcache, "kcache"), lse.data_ptr(), decay, weights.data_ptr(), stride)
+    return weights
+
+
+def k_paged_evict(plan: PagedPlan, kcache: torch.Tensor, vcache: torch.Tensor, weights: torch.Tensor, budget: int, first: int = 0,
+                  recent: int = 0, weights_out: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None):
+    """Every sequence of more than `budget` rows keeps, per key head, its first `first`, last `recent` and heaviest rows, moved to the
+    front of its pages; the kept rows' weights go to the front of weights_out (default: of weights).  Returns the kept positions
+    [n_seq][n_kv_head][budget], -1 behind the last."""
+    if kept is None:
+        kept = torch.empty((plan.n_seq, plan.n_kv_head, max(budget, 0)), dtype=torch.int32, device=plan.device)
+    elif kept.shape != (plan.n_seq, plan.n_kv_head, budget) or kept.dtype != torch.int32 or not kept.is_contiguous():
+        raise FloverError("kept: contiguous int32 [%d][%d][%d]" % (plan.n_seq, plan.n_kv_head, budget))
+    if weights_out is None:
+        weights_out = weights
+    stride = plan._weights(weights, plan.longest, "weights")
+    out_stride = stride if weights_out is weights else plan._weights(weights_out, min(budget, plan.longest), "weights_out")
+    stream = plan._on(kcache, vcache, weights, weights_out, kept)
+    plan._call(load_library().flover_k_paged_evict, stream, plan._cache(kcache, "kcache"), plan._cache(vcache, "vcache"),
+               weights.data_ptr(), stride, budget, first, recent, weights_out.data_ptr(), out_stride, kept.data_ptr())
+    return kept

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libflover.so")
-SOURCES = ["flover_api.hip", "kernels_gemm.hip", "kernels_elem.hip", "kernels_attn.hip"]
+SOURCES = ["flover_api.hip", "kernels_gemm.hip", "kernels_elem.hip", "kernels_attn.hip", "paged_api.hip",
+           "kernels_paged.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          # packed fp32 instructions are switched off for every kernel in this library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -31,7 +32,7 @@ def _compile(src: str) -> str:
 
 def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=4) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=6) as ex:
         objs = list(ex.map(_compile, SOURCES))
     subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
     if verbose:

@@ -17,6 +17,7 @@
 #include <string>
 #include <vector>
 
+#include "flover_error.h"
 #include "flover_kernels.h"
 
 namespace {
@@ -166,6 +167,9 @@ int fail(flover_ctx* c, int code, const std::string& msg) {
   }
   return code;
 }
+}  // namespace
+int flk::fail_call(int code, const std::string& msg) { return fail(nullptr, code, msg); }
+namespace {
 #define HIPCHK(ctx, expr)                                                                        \
   do {                                                                                           \
     hipError_t e_ = (expr);                                                                      \

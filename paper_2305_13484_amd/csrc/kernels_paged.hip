@@ -1,0 +1,598 @@
+// Operators on a cache kept in pages: rows of new tokens into it, their attention over it, the weights that attention gave to its
+// rows, and the eviction of the lightest.  A cache is [page][key head][page_size][d]; 16 consecutive positions of a sequence that start
+// at a multiple of 16 lie in one page, so whole 16-row groups of a wave share one entry of the page list, which a scalar load fetches.
+#include <algorithm>
+#include <cmath>
+
+#include "flover_dev.h"
+#include "paged.h"
+
+namespace flk {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Row of position pos (uniform in a wave) of a sequence in the cache of one key head.
+__device__ __forceinline__ uint32_t cache_row(const PagedView& v, const PagedSeq& s, int kvh, int pos) {
+  const int page = v.page_shift >= 0 ? pos >> v.page_shift : pos / v.page_size;
+  return ((uint32_t)v.pages[s.pages + page] * v.n_kv + kvh) * v.page_size + (uint32_t)(pos - page * v.page_size);
+}
+
+// ---------------------------------------------------------------- rows of new tokens
+
+// A thread moves 16 bytes of one key head's row of K or V (blockIdx.y).
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedView v, const char* __restrict__ k, int64_t ks, const char* __restrict__ vv,
+                                                           int64_t vs, char* __restrict__ kc, char* __restrict__ vc, int row_pieces) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int per_token = v.n_kv * row_pieces;
+  const int t = (int)(i / per_token);
+  if (t >= v.tokens) return;
+  const int rest = (int)(i - (int64_t)t * per_token), h = rest / row_pieces, piece = rest - h * row_pieces;
+  const size_t to = ((size_t)v.places[t] + (size_t)h * v.page_size) * row_pieces + piece;
+  if (blockIdx.y == 0) ((u32x4_t*)kc)[to] = *(const u32x4_t*)(k + t * ks + (size_t)rest * 16);
+  else ((u32x4_t*)vc)[to] = *(const u32x4_t*)(vv + t * vs + (size_t)rest * 16);
+}
+
+// ---------------------------------------------------------------- attention, few rows per key head
+
+__device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// Two storage elements packed in a dword (or one of fp32) with those that are not finite replaced by zero.
+template <int DT> __device__ __forceinline__ uint32_t finite_only(uint32_t x) {
+  if constexpr (DT == DT_F32) return (x & 0x7f800000u) == 0x7f800000u ? 0u : x;
+  constexpr uint32_t E = DT == DT_F16 ? 0x7c00u : 0x7f80u;
+  if ((x & E) == E) x &= 0xffff0000u;
+  if ((x & (E << 16)) == (E << 16)) x &= 0xffffu;
+  return x;
+}
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// permutation of a V row's 16-byte pieces (pairs stay together), so that the keys of a transposing read spread over the banks
+template <int D> __device__ __forceinline__ int piece_swizzle(int key) { return D == 128 ? (key & 7) * 2 : ((key >> 1) & 3) * 2; }
+
+template <int DT> __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+  if constexpr (DT == DT_BF16) return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16);
+  else return (uint32_t)f32_to_f16(a) | ((uint32_t)f32_to_f16(b) << 16);
+}
+
+// Four V^T operands (8 keys of 16 d each) by transposing reads; a[i]: this lane's LDS address of operand i, the second 16 keys lie HI
+// bytes further.  Its own wait stands in the block.
+template <int HI> __device__ __forceinline__ void read_keys_of_d(const uint32_t (&a)[4], u32x4_t (&v)[4]) {
+  uint2 x[4], y[4];
+  asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
+               "ds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
+               "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %6, %10 offset:%12\n\t"
+               "ds_read_b64_tr_b16 %3, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(HI)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = u32x4_t{x[i].x, x[i].y, y[i].x, y[i].y};
+}
+
+// One item: 16 query rows of a key head (row r = token r / group of the sequence's new ones, head r % group of the group, so that
+// grouped heads share what is read), its four waves taking every fourth step of KT keys; their results are merged through LDS.  The cache is
+// read once, straight to registers, the next step's rows on their way while a step is worked on; a token's K and V rows cost 4 operations per
+// byte and head of the group, so memory bounds it up to the 16 rows.
+//   scores   S^T[key][row] = K . Q^T: a lane's 16 bytes are consecutive d of one key (of one row);
+//   softmax  running maximum and sum per row = per output column, 2 in base 2, fp32;
+//   output   O^T[d][row] += V^T . P^T: P^T is what the lane holds already; V^T through the wave's own piece of LDS, 16-bit types by
+//            transposing reads.  P of 16-bit types enters as two terms, value and rounding remainder (16 bits or more together): memory
+//            leaves the time for it.
+// Keys that a row does not see have weight zero; if the sum comes out infinite or as no number all the same, it may be such a key's V (0 x inf),
+// and the wave's steps are gone through again with those elements kept out of the product and added where they are seen.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const PagedItem* __restrict__ items, const char* __restrict__ q,
+                                                         int64_t qs, const char* __restrict__ kc, const char* __restrict__ vc,
+                                                         void* __restrict__ out, float* __restrict__ lse) {
+  constexpr int EB = DT == DT_F32 ? 4 : 2, RB = D * EB;       // bytes of an element, of a row
+  constexpr int KT = DT == DT_F32 ? 16 : 32, KG = KT / 16;
+  constexpr int KS = RB / 64;               // 64-byte steps over a row
+  constexpr int LPR = RB / 16, RPI = 64 / LPR, NV = KT / RPI;  // V: lanes per row, rows per load, loads of a step
+  constexpr int DTL = D / 16;
+  constexpr int LD = D + 4;                 // floats per row of the merge, and of fp32 V
+  constexpr int WAVE_LDS = 16 * LD * 4;
+  static_assert(WAVE_LDS >= KT * RB, "a step of 16-bit V");
+  __shared__ __attribute__((aligned(256))) char lds[4][WAVE_LDS];
+  static_assert(WAVE_LDS % 256 == 0, "the operands' addresses are told apart by exclusive ors within a row");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, n = lane & 15;
+  const int kvh = blockIdx.x % v.n_kv;
+  const PagedItem it = items[blockIdx.x / v.n_kv];
+  const PagedSeq s = v.seqs[it.seq];
+  const int rows = s.fresh * v.group;
+  const int row = min(it.row0 + n, rows - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
+  const int qpos = s.len - s.fresh + token;                    // sees keys [qlo, qpos] and those below sinks
+  const int qlo = v.window > 0 ? qpos - v.window + 1 : 0;
+  const int last16 = (s.len - 1) & ~15;
+
+  u32x4_t qf[KS];
+  const char* qr = q + (s.first + token) * qs + (size_t)head * RB + g * 16;
+#pragma unroll
+  for (int i = 0; i < KS; ++i) qf[i] = *(const u32x4_t*)(qr + i * 64);
+  const float c = v.scale * kLog2e;
+
+  auto step_key = [&](int u) { return (u < it.gap ? u : u + it.skip) * KT; };
+  // rows behind the last repeat it (hidden below)
+  auto load = [&](u32x4_t(&kf)[KG][KS], u32x4_t(&vr)[NV], int u) {
+    const int k0 = step_key(u);
+#pragma unroll
+    for (int kg = 0; kg < KG; ++kg) {
+      const int p = min(k0 + kg * 16, last16);
+      const uint32_t r0 = cache_row(v, s, kvh, p);
+      const int most = s.len - 1 - p;
+      const char* kp = kc + (size_t)(r0 + min(n, most)) * RB + g * 16;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) kf[kg][i] = *(const u32x4_t*)(kp + i * 64);
+#pragma unroll
+      for (int j = kg * 16 / RPI; j < (kg + 1) * 16 / RPI; ++j)
+        vr[j] = *(const u32x4_t*)(vc + (size_t)(r0 + min(j * RPI - kg * 16 + lane / LPR, most)) * RB + lane % LPR * 16);
+    }
+  };
+
+  f32x4_t oacc[DTL];
+  float m, l;
+  char* mine = lds[wave];
+  const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+  const int vk = 4 * g + (n >> 2);
+  const uint32_t vaddr = mine_at + (uint32_t)((vk * LPR + (((n & 3) >> 1) ^ piece_swizzle<D>(vk))) * 16 + (n & 1) * 8);
+
+  auto consume = [&](const u32x4_t(&kf)[KG][KS], u32x4_t(&vr)[NV], int u, bool careful) {
+    const int k0 = step_key(u);
+    if (careful) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vr[j][e] = finite_only<DT>(vr[j][e]);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int r = j * RPI + lane / LPR, seg = lane % LPR;
+      if constexpr (DT == DT_F32) *(u32x4_t*)(mine + r * LD * 4 + seg * 16) = vr[j];
+      else *(u32x4_t*)(mine + (r * LPR + (seg ^ piece_swizzle<D>(r))) * 16) = vr[j];
+    }
+    float p[KG * 4], top = -INFINITY;
+#pragma unroll
+    for (int kg = 0; kg < KG; ++kg) {
+      f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        if constexpr (DT == DT_F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sacc = mfma_f32(__uint_as_float(kf[kg][i][e]), __uint_as_float(qf[i][e]), sacc);
+        } else {
+          sacc = mfma16<DT>(kf[kg][i], qf[i], sacc);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = k0 + kg * 16 + 4 * g + r;
+        const bool seen = key <= qpos && (key >= qlo || key < v.sinks);
+        p[kg * 4 + r] = seen ? sacc[r] * c : -INFINITY;
+        top = fmaxf(top, p[kg * 4 + r]);
+      }
+    }
+    top = max_partner<32>(max_partner<16>(top));
+    const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn;
+    const float alpha = __builtin_amdgcn_exp2f(m - ms);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int j = 0; j < KG * 4; ++j) {
+      p[j] = __builtin_amdgcn_exp2f(p[j] - ms);
+      l += p[j];                                               // this lane's share
+    }
+#pragma unroll
+    for (int dt = 0; dt < DTL; ++dt) oacc[dt] *= alpha;
+    if constexpr (DT == DT_F32) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int dt = 0; dt < DTL; ++dt)
+          oacc[dt] = mfma_f32(*(const float*)(mine + ((4 * g + r) * LD + dt * 16 + n) * 4), p[r], oacc[dt]);
+    } else {
+      float rest[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rest[j] = p[j] - rdt<DT>(p[j]);
+      const u32x4_t hi = {pack_pair<DT>(p[0], p[1]), pack_pair<DT>(p[2], p[3]), pack_pair<DT>(p[4], p[5]), pack_pair<DT>(p[6], p[7])};
+      const u32x4_t lo = {pack_pair<DT>(rest[0], rest[1]), pack_pair<DT>(rest[2], rest[3]), pack_pair<DT>(rest[4], rest[5]),
+                          pack_pair<DT>(rest[6], rest[7])};
+#pragma unroll
+      for (int d4 = 0; d4 < DTL; d4 += 4) {
+        uint32_t at[4];
+        u32x4_t va[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = vaddr ^ ((d4 + i) * 32);
+        read_keys_of_d<16 * RB>(at, va);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          oacc[d4 + i] = mfma16<DT>(va[i], lo, oacc[d4 + i]);
+          oacc[d4 + i] = mfma16<DT>(va[i], hi, oacc[d4 + i]);
+        }
+      }
+    }
+    if (careful) {
+      for (int j = 0; j < KT; ++j) {
+        const int key = k0 + j;
+        if (key >= s.len) break;
+        const uint32_t r = cache_row(v, s, kvh, key & ~15) + (key & 15);
+        const bool seen = key <= qpos && (key >= qlo || key < v.sinks);
+#pragma unroll
+        for (int dt = 0; dt < DTL; ++dt) {
+          const f32x4_t x = ldv4<DT>(vc, (size_t)r * D + dt * 16 + 4 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (seen && !is_finite(x[e])) oacc[dt][e] += x[e];
+        }
+      }
+    }
+  };
+
+  for (int pass = 0; pass < 2; ++pass) {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DTL; ++dt) oacc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    int u = it.u0 + wave;
+    if (u < it.u1) {
+      u32x4_t ka[KG][KS], va[NV], kb[KG][KS], vb[NV];
+      load(ka, va, u);
+      for (; u + 8 < it.u1; u += 8) {
+        load(kb, vb, u + 4);
+        consume(ka, va, u, pass);
+        load(ka, va, u + 8);
+        consume(kb, vb, u + 4, pass);
+      }
+      const bool two = u + 4 < it.u1;
+      if (two) load(kb, vb, u + 4);
+      consume(ka, va, u, pass);
+      if (two) consume(kb, vb, u + 4, pass);
+    }
+    bool fine = true;
+#pragma unroll
+    for (int dt = 0; dt < DTL; ++dt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) fine = fine && is_finite(oacc[dt][e]);
+    if (__all(fine)) break;
+  }
+
+  // the waves' results of a row, in the order of the waves
+  l = sum_partner<32>(sum_partner<16>(l));
+  __syncthreads();
+  float* my = (float*)mine + n * LD;
+#pragma unroll
+  for (int dt = 0; dt < DTL; ++dt) *(f32x4_t*)(my + dt * 16 + 4 * g) = oacc[dt];
+  if (g == 0) {
+    my[D] = m;
+    my[D + 1] = l;
+  }
+  __syncthreads();
+  const int r = threadIdx.x >> 4, i = threadIdx.x & 15;
+  if (it.row0 + r >= rows) return;
+  const float* from = (const float*)lds + r * LD;
+  constexpr int W = WAVE_LDS / 4;
+  const float mt = fmaxf(fmaxf(from[D], from[W + D]), fmaxf(from[2 * W + D], from[3 * W + D])), ms = mt == -INFINITY ? 0.f : mt;
+  float lt = 0.f;
+  f32x4_t o[D / 64];
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) o[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float a = __builtin_amdgcn_exp2f(from[w * W + D] - ms);
+    lt = fmaf(a, from[w * W + D + 1], lt);
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) o[e] += a * ld4(from + w * W + i * (D / 16) + e * 4);
+  }
+  const int tk = (it.row0 + r) / v.group, hd = kvh * v.group + it.row0 + r - tk * v.group;
+  if (it.part < 0) {
+    const size_t at = (size_t)(s.first + tk) * v.n_head + hd;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) stv4<DT>(out, at * D + i * (D / 16) + e * 4, o[e] / lt);
+    if (lse && i == 0) lse[at] = mt * kLn2 + logf(lt);
+  } else {
+    const size_t at = ((size_t)it.part * v.n_kv + kvh) * kRowTile + r;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) *(f32x4_t*)(v.po + at * D + i * (D / 16) + e * 4) = o[e];
+    if (i == 0) *(float2*)(v.pm + at * 2) = make_float2(mt, lt);
+  }
+}
+
+// Rows whose keys went to several items: block = (rows, key head), 16 threads a row, parts in their order.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedView v, const PagedMerge* __restrict__ merges, void* __restrict__ out,
+                                                          float* __restrict__ lse) {
+  const int kvh = blockIdx.x % v.n_kv;
+  const PagedMerge mg = merges[blockIdx.x / v.n_kv];
+  const PagedSeq s = v.seqs[mg.seq];
+  const int r = threadIdx.x >> 4, i = threadIdx.x & 15;
+  if (mg.row0 + r >= s.fresh * v.group) return;
+  const size_t first = ((size_t)mg.part0 * v.n_kv + kvh) * kRowTile + r, stride = (size_t)v.n_kv * kRowTile;
+  float mt = -INFINITY;
+  for (int p = i; p < mg.parts; p += 16) mt = fmaxf(mt, v.pm[(first + p * stride) * 2]);
+  mt = fmaxf(mt, partner<1>(mt));
+  mt = fmaxf(mt, partner<2>(mt));
+  mt = fmaxf(mt, partner<4>(mt));
+  mt = fmaxf(mt, partner<8>(mt));
+  const float ms = mt == -INFINITY ? 0.f : mt;
+  float lt = 0.f;
+  f32x4_t o[D / 64];
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) o[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < mg.parts; ++p) {
+    const float2 ml = *(const float2*)(v.pm + (first + p * stride) * 2);
+    const float a = __builtin_amdgcn_exp2f(ml.x - ms);
+    lt = fmaf(a, ml.y, lt);
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) o[e] += a * ld4(v.po + (first + p * stride) * D + i * (D / 16) + e * 4);
+  }
+  const int tk = (mg.row0 + r) / v.group, hd = kvh * v.group + mg.row0 + r - tk * v.group;
+  const size_t at = (size_t)(s.first + tk) * v.n_head + hd;
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) stv4<DT>(out, at * D + i * (D / 16) + e * 4, o[e] / lt);
+  if (lse && i == 0) lse[at] = mt * kLn2 + logf(lt);
+}
+
+// ---------------------------------------------------------------- weights that the new tokens gave to the cached rows
+
+// grid = (blocks of 256 positions, n_kv, n_seq); a wave holds the K rows of 64 positions and goes through the rows of queries that see any of
+// them, 16 at a time: S[row][key] = Q . K^T leaves a key's scores in one column, so that their exponentials add up in a lane.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void paged_weights_kernel(PagedView v, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc,
+                                                            const float* __restrict__ lse, float decay, float* __restrict__ w, int64_t ws) {
+  constexpr int EB = DT == DT_F32 ? 4 : 2, RB = D * EB, KS = RB / 64;
+  constexpr int KG = DT == DT_F32 ? 2 : 4;                     // 16-key groups held at a time
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, n = lane & 15, kvh = blockIdx.y;
+  const PagedSeq s = v.seqs[blockIdx.z];
+  const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
+  const float c = v.scale * kLog2e;
+  for (int half = 0; half < 4 / KG; ++half) {
+    const int k0 = blockIdx.x * 256 + wave * 64 + half * KG * 16;
+    if (k0 >= s.len) return;
+    const int k1 = min(k0 + KG * 16, s.len);                   // keys [k0, k1)
+    // new tokens that see some of them: [t0, t1)
+    const int t0 = max(0, k0 - before);
+    const int t1 = v.window > 0 && k0 >= v.sinks ? min(s.fresh, k1 - 1 + v.window - before) : s.fresh;
+    float sum[KG];
+#pragma unroll
+    for (int kg = 0; kg < KG; ++kg) sum[kg] = 0.f;
+    if (t0 < t1) {
+      u32x4_t kf[KG][KS];
+#pragma unroll
+      for (int kg = 0; kg < KG; ++kg) {
+        const int p = min(k0 + kg * 16, last16);
+        const char* kp = kc + (size_t)(cache_row(v, s, kvh, p) + min(n, s.len - 1 - p)) * RB + g * 16;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) kf[kg][i] = *(const u32x4_t*)(kp + i * 64);
+      }
+      const int r1 = t1 * v.group;
+      for (int r0 = t0 * v.group; r0 < r1; r0 += 16) {
+        const int row = min(r0 + n, r1 - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
+        const char* qr = q + (s.first + token) * qs + (size_t)head * RB + g * 16;
+        u32x4_t qf[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) qf[i] = *(const u32x4_t*)(qr + i * 64);
+        float base[4];                                         // of rows r0 + 4g + r: lse in base 2, and the position
+        int at[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int rr = min(r0 + 4 * g + r, r1 - 1), tk = rr / v.group;
+          base[r] = lse[(size_t)(s.first + tk) * v.n_head + kvh * v.group + rr - tk * v.group] * kLog2e;
+          at[r] = r0 + 4 * g + r < r1 ? before + tk : -1;      // -1: no such row
+        }
+#pragma unroll
+        for (int kg = 0; kg < KG; ++kg) {
+          f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < KS; ++i) {
+            if constexpr (DT == DT_F32) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sacc = mfma_f32(__uint_as_float(qf[i][e]), __uint_as_float(kf[kg][i][e]), sacc);
+            } else {
+              sacc = mfma16<DT>(qf[i], kf[kg][i], sacc);
+            }
+          }
+          const int key = k0 + kg * 16 + n;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool seen = key <= at[r] && (v.window <= 0 || key > at[r] - v.window || key < v.sinks);
+            sum[kg] += seen ? __builtin_amdgcn_exp2f(fmaf(sacc[r], c, -base[r])) : 0.f;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int kg = 0; kg < KG; ++kg) {
+      const float t = sum_partner<32>(sum_partner<16>(sum[kg]));
+      const int key = k0 + kg * 16 + n;
+      if (g == kg % 4 && key < s.len) {
+        float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + key;
+        *to = decay == 0.f || key >= before ? t : fmaf(decay, *to, t);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- eviction
+
+// Order of a weight: larger is heavier, NaN the lightest, both zeros alike.
+__device__ __forceinline__ uint32_t weight_key(float w) {
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+// A block per (key head, sequence).  The weight of the last row kept is found digit by digit from the top (four digits of 8 bits, counted
+// in LDS); rows of exactly that weight are taken from the front.  Then the positions are gone through in order, 1024 at a time, and numbered.
+__global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const float* w, int64_t ws, int budget, int first,
+                                                            int recent, float* wo, int64_t os, int* __restrict__ kept) {
+  __shared__ int count[256];
+  __shared__ int found[2];                 // digit, rows still wanted of it
+  __shared__ int waves[16][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const size_t at = (size_t)blockIdx.y * v.n_kv + blockIdx.x;
+  const int len = v.seqs[blockIdx.y].len;
+  const float* mine = w + at * ws;
+  float* to = wo ? wo + at * os : nullptr;
+  int* keep = kept + at * budget;
+  if (len <= budget) {
+    for (int p = tid; p < budget; p += 1024) {
+      keep[p] = p < len ? p : -1;
+      if (to && p < len && (wo != w)) to[p] = mine[p];
+    }
+    return;
+  }
+  const int sure = first + recent;         // of the others, `wanted` are kept
+  int wanted = budget - sure;
+  uint32_t prefix = 0;
+  for (int shift = 24; shift >= 0 && wanted > 0; shift -= 8) {
+    if (tid < 256) count[tid] = 0;
+    __syncthreads();
+    for (int p = first + tid; p < len - recent; p += 1024) {
+      const uint32_t k = weight_key(mine[p]);
+      if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&count[k >> shift & 255], 1);
+    }
+    __syncthreads();
+    if (wave == 0) {                       // lane l: digits 255 - 4l and the three below
+      int c[4], sum = 0;
+      for (int i = 0; i < 4; ++i) sum += c[i] = count[255 - 4 * lane - i];
+      int upto = sum;
+      for (int dlt = 1; dlt < 64; dlt <<= 1) {
+        const int o = __shfl_up(upto, dlt, 64);
+        if (lane >= dlt) upto += o;
+      }
+      if (lane == __builtin_ctzll(__ballot(upto >= wanted))) {      // the rows under way are more than `wanted`
+        int left = wanted - (upto - sum), i = 0;
+        while (i < 3 && c[i] < left) left -= c[i++];
+        found[0] = 255 - 4 * lane - i;
+        found[1] = left;
+      }
+    }
+    __syncthreads();
+    prefix |= (uint32_t)found[0] << shift;
+    wanted = found[1];
+    __syncthreads();
+  }
+  // heavier than prefix: kept; equal: the first `wanted`
+  int ranks = 0, ties = 0;                 // kept, and equal ones met, so far
+  for (int p0 = 0; p0 < len; p0 += 1024) {
+    const int p = p0 + tid;
+    const float x = p < len ? mine[p] : 0.f;
+    const bool certain = p < len && (p < first || p >= len - recent);
+    const bool middle = p < len && !certain && budget > sure;
+    const uint32_t k = weight_key(x);
+    const bool tie = middle && k == prefix;
+    const uint64_t tb = __ballot(tie);
+    const uint64_t below = (1ull << lane) - 1;
+    if (lane == 0) waves[wave][0] = __popcll(tb);
+    __syncthreads();
+    int t = ties;
+    for (int i = 0; i < 16; ++i) {
+      if (i < wave) t += waves[i][0];
+      ties += waves[i][0];
+    }
+    const bool take = certain || (middle && k > prefix) || (tie && t + __popcll(tb & below) < wanted);
+    const uint64_t kb = __ballot(take);
+    if (lane == 0) waves[wave][1] = __popcll(kb);
+    __syncthreads();
+    int r = ranks;
+    for (int i = 0; i < 16; ++i) {
+      if (i < wave) r += waves[i][1];
+      ranks += waves[i][1];
+    }
+    r += __popcll(kb & below);
+    if (take) {
+      keep[r] = p;
+      if (to) to[r] = x;                   // at or in front of p: behind the barriers nobody reads that place any more
+    }
+  }
+}
+
+// The kept rows to the front: block = (128 bytes of a row, key head, sequence x K|V), 256 threads, 8 per row, kMove rows of each thread at a time.
+// A row moves to a place at or in front of its own, and a place is overwritten only once every row up to it has been read: a
+// barrier between the reads (waited for) and the writes of a batch is enough, because the batch behind reads from places behind.
+constexpr int kMove = 8;
+__global__ __launch_bounds__(256) void paged_move_kernel(PagedView v, char* kc, char* vc, int budget, int first,
+                                                         const int* __restrict__ kept, int row_bytes) {
+  const PagedSeq s = v.seqs[blockIdx.z >> 1];
+  if (s.len <= budget) return;
+  const int kvh = blockIdx.y;
+  char* cache = (blockIdx.z & 1 ? vc : kc) + blockIdx.x * 128 + (threadIdx.x & 7) * 16;
+  const int* keep = kept + ((size_t)(blockIdx.z >> 1) * v.n_kv + kvh) * budget;
+  for (int r0 = first; r0 < budget; r0 += 32 * kMove) {
+    u32x4_t x[kMove];
+    int src[kMove];
+#pragma unroll
+    for (int j = 0; j < kMove; ++j) {
+      const int r = r0 + j * 32 + (threadIdx.x >> 3);
+      src[j] = r < budget ? keep[r] : r;
+    }
+#pragma unroll
+    for (int j = 0; j < kMove; ++j) {
+      const int r = r0 + j * 32 + (threadIdx.x >> 3);
+      if (src[j] != r) x[j] = *(const u32x4_t*)(cache + (size_t)cache_row(v, s, kvh, src[j]) * row_bytes);
+    }
+    copies_barrier<0>(true);
+#pragma unroll
+    for (int j = 0; j < kMove; ++j) {
+      const int r = r0 + j * 32 + (threadIdx.x >> 3);
+      if (src[j] != r) *(u32x4_t*)(cache + (size_t)cache_row(v, s, kvh, r) * row_bytes) = x[j];
+    }
+  }
+}
+
+// f(std::integral_constant dtype, head_dim)
+template <class F> void with_types(int dtype, int d, F f) {
+  auto wide = [&](auto dt) {
+    if (d == 128) f(dt, std::integral_constant<int, 128>{});
+    else f(dt, std::integral_constant<int, 64>{});
+  };
+  if (dtype == DT_F32) wide(std::integral_constant<int, DT_F32>{});
+  else if (dtype == DT_F16) wide(std::integral_constant<int, DT_F16>{});
+  else wide(std::integral_constant<int, DT_BF16>{});
+}
+int element_bytes(int dtype) { return dtype == DT_F32 ? 4 : 2; }
+
+}  // namespace
+
+hipError_t paged_append(int dtype, const PagedView& v, const void* k, int64_t ks, const void* vv, int64_t vs, void* kc, void* vc, hipStream_t st) {
+  const int eb = element_bytes(dtype), pieces = v.d * eb / 16;
+  const int64_t blocks = ((int64_t)v.tokens * v.n_kv * pieces + 255) / 256;
+  paged_append_kernel<<<dim3((unsigned)blocks, 2), 256, 0, st>>>(v, (const char*)k, ks * eb, (const char*)vv, vs * eb, (char*)kc, (char*)vc, pieces);
+  return hipGetLastError();
+}
+
+hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedMerge* merges, int n_merges,
+                           const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st) {
+  with_types(dtype, v.d, [&](auto dt, auto d) {
+    constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
+    if (n_rows) paged_rows_kernel<DT, D><<<n_rows * v.n_kv, 256, 0, st>>>(v, rows, (const char*)q, qs * element_bytes(DT), (const char*)kc,
+                                                                          (const char*)vc, out, lse);
+    if (n_merges) paged_merge_kernel<DT, D><<<n_merges * v.n_kv, 256, 0, st>>>(v, merges, out, lse);
+  });
+  return hipGetLastError();
+}
+
+hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t qs, const void* kc, const float* lse, float decay, float* w,
+                         int64_t ws, hipStream_t st) {
+  with_types(dtype, v.d, [&](auto dt, auto d) {
+    constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
+    paged_weights_kernel<DT, D><<<dim3((v.longest + 255) / 256, v.n_kv, v.n_seq), 256, 0, st>>>(
+        v, (const char*)q, qs * element_bytes(DT), (const char*)kc, lse, decay, w, ws);
+  });
+  return hipGetLastError();
+}
+
+hipError_t paged_evict(int dtype, const PagedView& v, void* kc, void* vc, const float* w, int64_t ws, int budget, int first, int recent,
+                       float* wo, int64_t os, int* kept, hipStream_t st) {
+  paged_select_kernel<<<dim3(v.n_kv, v.n_seq), 1024, 0, st>>>(v, w, ws, budget, first, recent, wo, os, kept);
+  const int row_bytes = v.d * element_bytes(dtype);
+  if (v.longest > budget)
+    paged_move_kernel<<<dim3(row_bytes / 128, v.n_kv, 2 * v.n_seq), 256, 0, st>>>(v, (char*)kc, (char*)vc, budget, first, kept, row_bytes);
+  return hipGetLastError();
+}
+
+}  // namespace flk

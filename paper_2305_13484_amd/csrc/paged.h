@@ -1,0 +1,49 @@
+// Operators on a cache kept in pages: what the host side (paged_api.hip) hands to the kernels (kernels_paged.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace flk {
+
+constexpr int kRowTile = 16;        // query rows (token x head of a group) of a block of the streaming kernel
+inline int row_keys(int dtype) { return dtype == 0 ? 16 : 32; }    // keys of a step of it: 32 of 16-bit caches, 16 of fp32 ones
+
+// A sequence of the plan.
+struct PagedSeq {
+  int first;      // its first new token's row in q, k, v and out
+  int fresh;      // new tokens
+  int len;        // cached rows with them
+  int pages;      // its first entry in the page list
+};
+// A block's work: rows [row0, row0 + tile) of one key head of a sequence over steps [u0, u1) of the keys that some row sees.  Step u is
+// keys step * u .. while u < gap, and step * (u + skip) .. behind: the keys between first tokens and window are left out.
+struct PagedItem {
+  int seq, row0, u0, u1, gap, skip;
+  int part;       // where its partial result goes, -1: it has all keys, and writes the output
+  int pad;
+};
+// Rows whose keys are shared out to `parts` items.
+struct PagedMerge {
+  int seq, row0, part0, parts;
+};
+
+struct PagedView {     // device memory of a plan, and the shape
+  const PagedSeq* seqs;
+  const int* pages;
+  const uint32_t* places;      // [T] row of a new token in the cache, key head 0
+  float *pm, *po;              // partial results [part][key head][tile]: (max, sum), [head_dim]
+  int n_seq, tokens, longest;
+  int n_head, n_kv, group, d, page_size, page_shift;   // page_shift -1: page_size is not a power of two
+  int window, sinks;
+  float scale;
+};
+
+hipError_t paged_append(int dtype, const PagedView& v, const void* k, int64_t ks, const void* vv, int64_t vs, void* kc, void* vc, hipStream_t st);
+hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedMerge* merges, int n_merges,
+                           const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st);
+hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t qs, const void* kc, const float* lse, float decay, float* w,
+                         int64_t ws, hipStream_t st);
+hipError_t paged_evict(int dtype, const PagedView& v, void* kc, void* vc, const float* w, int64_t ws, int budget, int first, int recent,
+                       float* wo, int64_t os, int* kept, hipStream_t st);
+
+}  // namespace flk
