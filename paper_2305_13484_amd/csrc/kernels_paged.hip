@@ -292,10 +292,229 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
     for (int e = 0; e < D / 64; ++e) stv4<DT>(out, at * D + i * (D / 16) + e * 4, o[e] / lt);
     if (lse && i == 0) lse[at] = mt * kLn2 + logf(lt);
   } else {
-    const size_t at = ((size_t)it.part * v.n_kv + kvh) * kRowTile + r;
+    const size_t at = (size_t)it.part + kvh * kRowTile + r;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) *(f32x4_t*)(v.po + at * D + i * (D / 16) + e * 4) = o[e];
     if (i == 0) *(float2*)(v.pm + at * 2) = make_float2(mt, lt);
+  }
+}
+
+// ---------------------------------------------------------------- attention, many rows per key head
+
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+
+// D[32][32] += A[32][16] . B[16][32]: a lane holds row (column) lane % 32 of A (B), 8 consecutive k from 8 * (lane / 32), and of D column lane % 32,
+// rows i % 4 + 8 * (i / 4) + 4 * (lane / 32), i < 16
+template <int DT> __device__ __forceinline__ f32x16_t mfma32(const u32x4_t& a, const u32x4_t& b, f32x16_t c) {
+  if constexpr (DT == DT_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+template <int DT> __device__ __forceinline__ uint32_t round_pair(float a, float b) {      // to nearest even
+  if constexpr (DT == DT_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+  else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
+}
+// V^T operands of 16 keys and D / 32 times 32 d by transposing reads: 16 lanes give the addresses of 4 keys x 16 d and get 4 keys of one d
+// each; the second four keys of a lane lie HI bytes further.  Its own wait stands in the block.
+template <int HI> __device__ __forceinline__ void read_keys_of_32d(const uint32_t (&a)[2], u32x4_t (&v)[2]) {
+  uint2 x[2], y[2];
+  asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %2, %4 offset:%6\n\t"
+               "ds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\t"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(y[0]), "=&v"(y[1])
+               : "v"(a[0]), "v"(a[1]), "n"(HI)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 2; ++i) v[i] = u32x4_t{x[i].x, x[i].y, y[i].x, y[i].y};
+}
+template <int HI> __device__ __forceinline__ void read_keys_of_32d(const uint32_t (&a)[4], u32x4_t (&v)[4]) { read_keys_of_d<HI>(a, v); }
+
+// One item of 128 query rows of a key head, 32 per wave; the block's waves share the keys, 64 at a time, the next 64 rows of K and V on their way
+// to LDS (asynchronous copies, two buffers) while the present ones are worked on.  16-bit types.
+//   scores   S^T[key][row] = K . Q^T in tiles of 32 x 32, so that a row's scores lie in two lanes;
+//   softmax  running maximum and sum per row in fp32.  The maximum follows only when a score passes it by 8 (in base 2): weights are up to
+//            2^8 then, and the sums are scaled again rarely;
+//   output   O^T[d][row] += V^T . P^T: P^T is what the lanes hold, rounded to the 16-bit type (half a step of the weight, like the
+//            output's own rounding; the sum in the denominator is of the unrounded ones); V^T by transposing reads.
+// LDS rows are the cache's, their 16-byte pieces permuted by key so that a read's keys spread over the banks.  Steps that every row of the wave
+// sees in full take no mask.  A sum that is infinite or no number: as in paged_rows_kernel, the block goes through its keys again.
+template <int DT, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_tile_kernel(
+    PagedView v, const PagedItem* __restrict__ items, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc,
+    const char* __restrict__ vc, void* __restrict__ out, float* __restrict__ lse) {
+  constexpr int RB = D * 2, KS = D / 16, DTL = D / 32, SEG = D / 8;      // row bytes, 16-d steps, 32-d tiles, 16-byte pieces of a row
+  constexpr int RPC = 64 / SEG, NC = 16 / RPC;                          // rows of a copy, copies of 16 rows
+  constexpr int BUF = kTileKeys * RB;
+  __shared__ __attribute__((aligned(1024))) char lds[2][2][BUF];        // [buffer][K | V]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, n = lane & 31;
+  const int kvh = blockIdx.x % v.n_kv;
+  const PagedItem it = items[blockIdx.x / v.n_kv];
+  const PagedSeq s = v.seqs[it.seq];
+  const int rows = s.fresh * v.group, before = s.len - s.fresh;
+  const int row0 = it.row0 + wave * 32;
+  const int row = min(row0 + n, rows - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
+  const int qpos = before + token, qlo = v.window > 0 ? qpos - v.window + 1 : 0;
+  // positions of the wave's rows: [p0, p1]
+  const int p0 = before + min(row0, rows - 1) / v.group, p1 = row0 < rows ? before + min(row0 + 31, rows - 1) / v.group : -1;
+  const int last16 = (s.len - 1) & ~15;
+  u32x4_t qf[KS];
+  const char* qr = q + (s.first + token) * qs + (size_t)head * RB + h * 16;
+#pragma unroll
+  for (int i = 0; i < KS; ++i) qf[i] = *(const u32x4_t*)(qr + i * 32);
+  const float c = v.scale * kLog2e;
+
+  auto step_key = [&](int u) { return (u < it.gap ? u : u + it.skip) * kTileKeys; };
+  // a wave copies rows 16 * wave .. + 15 of a step; rows behind the last repeat it (hidden below)
+  auto place_of = [&](int u) { return min(step_key(u) + wave * 16, last16); };
+  auto k_swizzle = [](int key) { return D == 128 ? key & 15 : (key >> 1) & 7; };
+  auto issue = [&](int u, uint32_t r0) {
+    char(*buf)[BUF] = lds[(u - it.u0) & 1];
+    const int most = s.len - 1 - place_of(u);
+    const char *kb = kc + (size_t)r0 * RB, *vb = vc + (size_t)r0 * RB;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int r = j * RPC + lane / SEG, key = wave * 16 + r, from = min(r, most) * RB;
+      copy_to_lds(kb, from + ((lane % SEG) ^ k_swizzle(key)) * 16, (u32x4_t*)(buf[0] + wave * 16 * RB + j * 1024));
+      copy_to_lds(vb, from + ((lane % SEG) ^ piece_swizzle<D>(key)) * 16, (u32x4_t*)(buf[1] + wave * 16 * RB + j * 1024));
+    }
+  };
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0];
+  // this lane's 8 bytes of V for the first operand: key 4h + i / 4, d 16 * (second 16 lanes) + 4 * (i % 4), i = lane % 16
+  const int vk = 4 * h + ((lane & 15) >> 2), vp = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const uint32_t vaddr = lds_at + BUF + (uint32_t)(vk * RB + (vp ^ piece_swizzle<D>(vk)) * 16 + (lane & 1) * 8);
+
+  f32x16_t oacc[DTL];
+  float m, l;                                 // the running maximum (of unscaled scores), this lane's share of the sum
+  auto consume = [&](int u, bool careful) {
+    const int k0 = step_key(u), b = (u - it.u0) & 1;
+    if (k0 > p1) return;                      // none of the wave's rows sees these keys
+    const bool full = k0 + kTileKeys - 1 <= p0 && (v.window <= 0 || k0 > p1 - v.window || k0 + kTileKeys <= v.sinks) && !careful;
+    f32x16_t sacc[2];
+    const char* kl = lds[b][0];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const char* kr = kl + (kt * 32 + n) * RB;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sacc[kt][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        sacc[kt] = mfma32<DT>(*(const u32x4_t*)(kr + (((ks * 2 + h) ^ k_swizzle(n)) * 16)), qf[ks], sacc[kt]);
+    }
+    if (!full) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = k0 + kt * 32 + (i & 3) + 8 * (i >> 2) + 4 * h;
+          if (!(key <= qpos && (key >= qlo || key < v.sinks))) sacc[kt][i] = -INFINITY;
+        }
+    }
+    float top = sacc[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, sacc[i >> 4][i & 15]);
+    top = max_partner<32>(top);
+    if (__any((top - m) * c > 8.f || (m == -INFINITY && top > m))) {
+      const float mn = fmaxf(m, top);
+      const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * c);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DTL; ++dt) oacc[dt] *= alpha;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(sacc[i >> 4][i & 15], c, -mc));
+      sacc[i >> 4][i & 15] = p;
+      l += p;
+    }
+#pragma unroll
+    for (int st = 0; st < 4; ++st) {           // 16 keys
+      u32x4_t pb;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pb[e] = round_pair<DT>(sacc[st >> 1][(st & 1) * 8 + 2 * e], sacc[st >> 1][(st & 1) * 8 + 2 * e + 1]);
+      uint32_t at[DTL];
+      u32x4_t va[DTL];
+#pragma unroll
+      for (int dt = 0; dt < DTL; ++dt) at[dt] = (vaddr + b * (2 * BUF) + st * 16 * RB) ^ (dt * 64);
+      read_keys_of_32d<8 * RB>(at, va);
+#pragma unroll
+      for (int dt = 0; dt < DTL; ++dt) {
+        if (careful) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) va[dt][e] = finite_only<DT>(va[dt][e]);
+        }
+        oacc[dt] = mfma32<DT>(va[dt], pb, oacc[dt]);
+      }
+    }
+    if (careful) {
+      for (int j = 0; j < kTileKeys; ++j) {
+        const int key = k0 + j;
+        if (key >= s.len) break;
+        const uint32_t r = cache_row(v, s, kvh, key & ~15) + (key & 15);
+        const bool seen = key <= qpos && (key >= qlo || key < v.sinks);
+#pragma unroll
+        for (int dt = 0; dt < DTL; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const f32x4_t x = ldv4<DT>(vc, (size_t)r * D + dt * 32 + 2 * i + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (seen && !is_finite(x[e])) oacc[dt][i + e] += x[e];
+          }
+      }
+    }
+  };
+
+  for (int pass = 0; pass < 2; ++pass) {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DTL; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
+    issue(it.u0, cache_row(v, s, kvh, place_of(it.u0)));
+    uint32_t next = it.u0 + 1 < it.u1 ? cache_row(v, s, kvh, place_of(it.u0 + 1)) : 0;
+    for (int u = it.u0; u < it.u1; ++u) {
+      copies_barrier<0>(true);                 // step u has landed; every wave is done with step u - 1
+      if (u + 1 < it.u1) issue(u + 1, next);
+      if (u + 2 < it.u1) next = cache_row(v, s, kvh, place_of(u + 2));
+      consume(u, pass);
+    }
+    bool fine = true;
+#pragma unroll
+    for (int dt = 0; dt < DTL; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) fine = fine && is_finite(oacc[dt][i]);
+    if (!__syncthreads_or(!fine)) break;       // (and behind it the buffers are free)
+  }
+
+  l = sum_partner<32>(l);
+  if (row0 + n >= rows) return;
+  const int tk = (row0 + n) / v.group;
+  if (it.part < 0) {
+    const size_t at = (size_t)(s.first + tk) * v.n_head + kvh * v.group + row0 + n - tk * v.group;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int dt = 0; dt < DTL; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        stv4<DT>(out, at * D + dt * 32 + 2 * i + 4 * h,
+                 f32x4_t{oacc[dt][i] * inv, oacc[dt][i + 1] * inv, oacc[dt][i + 2] * inv, oacc[dt][i + 3] * inv});
+    if (lse && h == 0) lse[at] = m * v.scale + logf(l);
+  } else {
+    const size_t at = (size_t)it.part + kvh * kTileRows + wave * 32 + n;
+#pragma unroll
+    for (int dt = 0; dt < DTL; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4_t*)(v.po + at * D + dt * 32 + 2 * i + 4 * h) = f32x4_t{oacc[dt][i], oacc[dt][i + 1], oacc[dt][i + 2], oacc[dt][i + 3]};
+    if (h == 0) *(float2*)(v.pm + at * 2) = make_float2(m * c, l);
   }
 }
 
@@ -308,7 +527,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedView v, const Pag
   const PagedSeq s = v.seqs[mg.seq];
   const int r = threadIdx.x >> 4, i = threadIdx.x & 15;
   if (mg.row0 + r >= s.fresh * v.group) return;
-  const size_t first = ((size_t)mg.part0 * v.n_kv + kvh) * kRowTile + r, stride = (size_t)v.n_kv * kRowTile;
+  const size_t first = (size_t)mg.part + kvh * mg.tile + r, stride = mg.stride;
   float mt = -INFINITY;
   for (int p = i; p < mg.parts; p += 16) mt = fmaxf(mt, v.pm[(first + p * stride) * 2]);
   mt = fmaxf(mt, partner<1>(mt));
@@ -565,10 +784,13 @@ hipError_t paged_append(int dtype, const PagedView& v, const void* k, int64_t ks
   return hipGetLastError();
 }
 
-hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedMerge* merges, int n_merges,
-                           const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st) {
+hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedItem* tiles, int n_tiles,
+                           const PagedMerge* merges, int n_merges, const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st) {
   with_types(dtype, v.d, [&](auto dt, auto d) {
     constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
+    if constexpr (DT != DT_F32)
+      if (n_tiles) paged_tile_kernel<DT, D><<<n_tiles * v.n_kv, 256, 0, st>>>(v, tiles, (const char*)q, qs * 2, (const char*)kc,
+                                                                              (const char*)vc, out, lse);
     if (n_rows) paged_rows_kernel<DT, D><<<n_rows * v.n_kv, 256, 0, st>>>(v, rows, (const char*)q, qs * element_bytes(DT), (const char*)kc,
                                                                           (const char*)vc, out, lse);
     if (n_merges) paged_merge_kernel<DT, D><<<n_merges * v.n_kv, 256, 0, st>>>(v, merges, out, lse);

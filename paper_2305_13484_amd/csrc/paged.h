@@ -7,6 +7,7 @@ namespace flk {
 
 constexpr int kRowTile = 16;        // query rows (token x head of a group) of a block of the streaming kernel
 inline int row_keys(int dtype) { return dtype == 0 ? 16 : 32; }    // keys of a step of it: 32 of 16-bit caches, 16 of fp32 ones
+constexpr int kTileRows = 128, kTileKeys = 64;                     // the same of the tile kernel (16-bit types)
 
 // A sequence of the plan.
 struct PagedSeq {
@@ -19,19 +20,20 @@ struct PagedSeq {
 // keys step * u .. while u < gap, and step * (u + skip) .. behind: the keys between first tokens and window are left out.
 struct PagedItem {
   int seq, row0, u0, u1, gap, skip;
-  int part;       // where its partial result goes, -1: it has all keys, and writes the output
+  int part;       // first row of its partial result (key head h: h * tile rows further), -1: it has all keys, and writes the output
   int pad;
 };
-// Rows whose keys are shared out to `parts` items.
+// Up to 16 rows whose keys are shared out to `parts` items: partial rows at `part`, `stride` rows from part to part, `tile` from key head to
+// key head.
 struct PagedMerge {
-  int seq, row0, part0, parts;
+  int seq, row0, part, stride, parts, tile;
 };
 
 struct PagedView {     // device memory of a plan, and the shape
   const PagedSeq* seqs;
   const int* pages;
   const uint32_t* places;      // [T] row of a new token in the cache, key head 0
-  float *pm, *po;              // partial results [part][key head][tile]: (max, sum), [head_dim]
+  float *pm, *po;              // partial results: (max, sum) of a row, its [head_dim]
   int n_seq, tokens, longest;
   int n_head, n_kv, group, d, page_size, page_shift;   // page_shift -1: page_size is not a power of two
   int window, sinks;
@@ -39,7 +41,7 @@ struct PagedView {     // device memory of a plan, and the shape
 };
 
 hipError_t paged_append(int dtype, const PagedView& v, const void* k, int64_t ks, const void* vv, int64_t vs, void* kc, void* vc, hipStream_t st);
-hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedMerge* merges, int n_merges,
+hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedItem* tiles, int n_tiles, const PagedMerge* merges, int n_merges,
                            const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st);
 hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t qs, const void* kc, const float* lse, float decay, float* w,
                          int64_t ws, hipStream_t st);

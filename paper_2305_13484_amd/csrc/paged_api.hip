@@ -59,14 +59,14 @@ int check_shape(const flover_paged_shape* s) {
 // A plan's lists as they go to the device, and where each begins.
 struct Lists {
   std::vector<char> bytes;
-  size_t pages = 0, places = 0, rows = 0, merges = 0;      // offsets; the sequences come first
+  size_t pages = 0, places = 0, rows = 0, tiles = 0, merges = 0;      // offsets; the sequences come first
   size_t pm = 0, po = 0, total = 0;                        // partial results, behind the lists
-  int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_merges = 0;
+  int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_tiles = 0, n_merges = 0;
   bool shared = false, shared_new = false;                 // a page twice in use; one that new tokens go to
 };
 
-// Blocks that a launch is cut into where sequences are few and long.
-constexpr int kBlocks = 768;
+// Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long.
+constexpr int kBlocks[2] = {768, 512};
 
 int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const int32_t* len, const int32_t* table, int stride, Lists* L) {
   auto bad = [](const std::string& m) { return fail_call(FLOVER_E_INVAL, m); };
@@ -123,40 +123,53 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   std::vector<int> order(n_seq);
   std::iota(order.begin(), order.end(), 0);
   std::sort(order.begin(), order.end(), [&](int a, int b) { return len[a] != len[b] ? len[a] > len[b] : a < b; });
-  std::vector<PagedItem> items;
-  for (int i : order) {
-    const int rows = new_len[i] * group, tile = flk::kRowTile, step = flk::row_keys(sh.dtype), before = len[i] - new_len[i];
-    for (int r0 = (rows - 1) / tile * tile; r0 >= 0 && rows > 0; r0 -= tile) {
-      const int lo = before + r0 / group, hi = before + (std::min(rows, r0 + tile) - 1) / group;      // positions of the rows
-      const int end = hi / step + 1;
-      int gap = 0, skip = 0;
-      if (sh.window > 0) {
-        const int from = std::max(0, lo - sh.window + 1) / step, heads = (int)std::min<int64_t>(from, ((int64_t)sh.sinks + step - 1) / step);
-        gap = heads;
-        skip = from - heads;
-      }
-      items.push_back({i, r0, 0, end - skip, gap, skip, -1, 0});
-    }
-  }
-  int64_t steps = 0;
-  for (const PagedItem& it : items) steps += it.u1;
-  const int64_t share = std::max<int64_t>(8, (steps * sh.n_kv_head + kBlocks - 1) / kBlocks);
-  std::vector<PagedItem> rows;
+  std::vector<PagedItem> rows, tiles;
   std::vector<PagedMerge> merges;
-  int part = 0;
-  for (const PagedItem& it : items) {
-    const int parts = it.u1 * 4LL <= share * 5 ? 1 : (int)((it.u1 + share - 1) / share);
-    if (parts > 1) merges.push_back({it.seq, it.row0, part, parts});
-    for (int p = 0; p < parts; ++p) {
-      PagedItem x = it;
-      x.u0 = (int)((int64_t)it.u1 * p / parts);
-      x.u1 = (int)((int64_t)it.u1 * (p + 1) / parts);
-      x.part = parts > 1 ? part++ : -1;
-      rows.push_back(x);
+  int64_t partial = 0;                                     // rows of partial results
+  for (int kind = 0; kind < 2; ++kind) {                   // the streaming kernel's work, the tile kernel's
+    const int tile = kind ? flk::kTileRows : flk::kRowTile, step = kind ? flk::kTileKeys : flk::row_keys(sh.dtype);
+    std::vector<PagedItem> items;
+    int64_t steps = 0;
+    for (int i : order) {
+      const int rows_of = new_len[i] * group, before = len[i] - new_len[i];
+      if (rows_of == 0 || (sh.dtype != FLOVER_F32 && rows_of > flk::kRowTile) != (kind == 1)) continue;
+      for (int r0 = (rows_of - 1) / tile * tile; r0 >= 0; r0 -= tile) {
+        const int lo = before + r0 / group, hi = before + (std::min(rows_of, r0 + tile) - 1) / group;      // positions of the rows
+        const int end = hi / step + 1;
+        int gap = 0, skip = 0;
+        if (sh.window > 0) {
+          const int from = std::max(0, lo - sh.window + 1) / step;
+          gap = (int)std::min<int64_t>(from, ((int64_t)sh.sinks + step - 1) / step);
+          skip = from - gap;
+        }
+        items.push_back({i, r0, 0, end - skip, gap, skip, -1, 0});
+        steps += end - skip;
+      }
+    }
+    const int64_t share = std::max<int64_t>(8, (steps * sh.n_kv_head + kBlocks[kind] - 1) / kBlocks[kind]);
+    std::vector<PagedItem>& to = kind ? tiles : rows;
+    for (const PagedItem& it : items) {
+      const int parts = it.u1 * 4LL <= share * 5 ? 1 : (int)((it.u1 + share - 1) / share);
+      if (parts > 1)
+        for (int r = 0; r < tile && it.row0 + r < new_len[it.seq] * group; r += 16)
+          merges.push_back({it.seq, it.row0 + r, (int)partial + r, tile * sh.n_kv_head, parts, tile});
+      for (int p = 0; p < parts; ++p) {
+        PagedItem x = it;
+        x.u0 = (int)((int64_t)it.u1 * p / parts);
+        x.u1 = (int)((int64_t)it.u1 * (p + 1) / parts);
+        x.part = -1;
+        if (parts > 1) {
+          x.part = (int)partial;
+          partial += (int64_t)tile * sh.n_kv_head;
+        }
+        to.push_back(x);
+      }
+      if (partial >= 2147483648LL) return bad("too many partial results");
     }
   }
-  if ((int64_t)rows.size() * sh.n_kv_head >= 2147483648LL) return bad("too much work for one launch");
+  if ((int64_t)(rows.size() + tiles.size() + merges.size()) * sh.n_kv_head >= 2147483648LL) return bad("too much work for one launch");
   L->n_rows = (int)rows.size();
+  L->n_tiles = (int)tiles.size();
   L->n_merges = (int)merges.size();
 
   size_t off = 0;
@@ -169,6 +182,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   L->pages = put(pages.size() * 4);
   L->places = put(places.size() * 4);
   L->rows = put(rows.size() * sizeof(PagedItem));
+  L->tiles = put(tiles.size() * sizeof(PagedItem));
   L->merges = put(merges.size() * sizeof(PagedMerge));
   L->bytes.assign(off, 0);
   auto fill = [&](size_t at, const void* from, size_t n) {
@@ -178,10 +192,10 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   fill(L->pages, pages.data(), pages.size() * 4);
   fill(L->places, places.data(), places.size() * 4);
   fill(L->rows, rows.data(), rows.size() * sizeof(PagedItem));
+  fill(L->tiles, tiles.data(), tiles.size() * sizeof(PagedItem));
   fill(L->merges, merges.data(), merges.size() * sizeof(PagedMerge));
-  const size_t partial = (size_t)part * sh.n_kv_head * flk::kRowTile;
-  L->pm = put(partial * 2 * 4);
-  L->po = put(partial * sh.head_dim * 4);
+  L->pm = put((size_t)partial * 2 * 4);
+  L->po = put((size_t)partial * sh.head_dim * 4);
   L->total = std::max<size_t>(off, 256);
   return FLOVER_OK;
 }
@@ -389,7 +403,7 @@ int32_t flover_k_paged_attention(const flover_paged_plan* plan, const void* q, i
     PAGED_TRY(ready(plan, (hipStream_t)stream));
     const Lists& l = plan->lists;
     PAGED_HIP(flk::paged_attention(plan->shape.dtype, plan->view(), (const PagedItem*)(plan->memory + l.rows), l.n_rows,
-                                   (const PagedMerge*)(plan->memory + l.merges), l.n_merges, q, q_stride, kcache, vcache, out, lse,
+                                   (const PagedItem*)(plan->memory + l.tiles), l.n_tiles, (const PagedMerge*)(plan->memory + l.merges), l.n_merges, q, q_stride, kcache, vcache, out, lse,
                                    (hipStream_t)stream));
     return FLOVER_OK;
   });
