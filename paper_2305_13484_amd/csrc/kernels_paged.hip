@@ -36,6 +36,13 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedView v, const ch
 
 // ---------------------------------------------------------------- attention, few rows per key head
 
+// 16 bytes of a cache row.  16-bit caches are read once by the streaming kernel (nothing to keep in the caches); of fp32 ones every 16 query
+// rows read them again.
+template <int DT> __device__ __forceinline__ u32x4_t load_rows(const char* p) {
+  if constexpr (DT == DT_F32) return *(const u32x4_t*)p;
+  else return __builtin_nontemporal_load((const u32x4_t*)p);
+}
+
 __device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // Two storage elements packed in a dword (or one of fp32) with those that are not finite replaced by zero.
@@ -84,7 +91,7 @@ template <int HI> __device__ __forceinline__ void read_keys_of_d(const uint32_t 
 // Keys that a row does not see have weight zero; if the sum comes out infinite or as no number all the same, it may be such a key's V (0 x inf),
 // and the wave's steps are gone through again with those elements kept out of the product and added where they are seen.
 template <int DT, int D>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const PagedItem* __restrict__ items, const char* __restrict__ q,
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_rows_kernel(PagedView v, const PagedItem* __restrict__ items, const char* __restrict__ q,
                                                          int64_t qs, const char* __restrict__ kc, const char* __restrict__ vc,
                                                          void* __restrict__ out, float* __restrict__ lse) {
   constexpr int EB = DT == DT_F32 ? 4 : 2, RB = D * EB;       // bytes of an element, of a row
@@ -92,11 +99,10 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
   constexpr int KS = RB / 64;               // 64-byte steps over a row
   constexpr int LPR = RB / 16, RPI = 64 / LPR, NV = KT / RPI;  // V: lanes per row, rows per load, loads of a step
   constexpr int DTL = D / 16;
-  constexpr int LD = D + 4;                 // floats per row of the merge, and of fp32 V
-  constexpr int WAVE_LDS = 16 * LD * 4;
-  static_assert(WAVE_LDS >= KT * RB, "a step of 16-bit V");
-  __shared__ __attribute__((aligned(256))) char lds[4][WAVE_LDS];
-  static_assert(WAVE_LDS % 256 == 0, "the operands' addresses are told apart by exclusive ors within a row");
+  constexpr int LD = D + 4;                 // floats per row of the merge
+  constexpr int STEP = KT * RB;             // bytes of a step of K, of V
+  __shared__ __attribute__((aligned(1024))) char lds[4][2 * STEP];      // [wave][K | V]
+  static_assert(2 * STEP >= 16 * LD * 4, "a wave's results");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15;
   const int kvh = blockIdx.x % v.n_kv;
@@ -115,32 +121,41 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
   const float c = v.scale * kLog2e;
 
   auto step_key = [&](int u) { return (u < it.gap ? u : u + it.skip) * KT; };
-  // rows behind the last repeat it (hidden below)
-  auto load = [&](u32x4_t(&kf)[KG][KS], u32x4_t(&vr)[NV], int u) {
-    const int k0 = step_key(u);
+  // rows of a step's 16-key groups in the cache; those behind the last repeat it (hidden below)
+  struct Place {
+    uint32_t row[KG];
+    int most[KG];
+  };
+  auto place_of = [&](int u) {
+    Place pl;
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) {
-      const int p = min(k0 + kg * 16, last16);
-      const uint32_t r0 = cache_row(v, s, kvh, p);
-      const int most = s.len - 1 - p;
-      const char* kp = kc + (size_t)(r0 + min(n, most)) * RB + g * 16;
+      const int p = min(step_key(u) + kg * 16, last16);
+      pl.row[kg] = cache_row(v, s, kvh, p);
+      pl.most[kg] = s.len - 1 - p;
+    }
+    return pl;
+  };
+  const int lr = lane / LPR, seg = lane % LPR;
+  auto load = [&](const Place& pl, u32x4_t(&kr)[NV], u32x4_t(&vr)[NV]) {
 #pragma unroll
-      for (int i = 0; i < KS; ++i) kf[kg][i] = *(const u32x4_t*)(kp + i * 64);
-#pragma unroll
-      for (int j = kg * 16 / RPI; j < (kg + 1) * 16 / RPI; ++j)
-        vr[j] = *(const u32x4_t*)(vc + (size_t)(r0 + min(j * RPI - kg * 16 + lane / LPR, most)) * RB + lane % LPR * 16);
+    for (int j = 0; j < NV; ++j) {
+      constexpr int G = 16 / RPI;             // loads of a group
+      const size_t at = (size_t)(pl.row[j / G] + min(j % G * RPI + lr, pl.most[j / G])) * RB + seg * 16;
+      kr[j] = load_rows<DT>(kc + at);
+      vr[j] = load_rows<DT>(vc + at);
     }
   };
 
   f32x4_t oacc[DTL];
   float m, l;
-  char* mine = lds[wave];
-  const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+  char *mk = lds[wave], *mv = lds[wave] + STEP;
   const int vk = 4 * g + (n >> 2);
-  const uint32_t vaddr = mine_at + (uint32_t)((vk * LPR + (((n & 3) >> 1) ^ piece_swizzle<D>(vk))) * 16 + (n & 1) * 8);
-
-  auto consume = [&](const u32x4_t(&kf)[KG][KS], u32x4_t(&vr)[NV], int u, bool careful) {
-    const int k0 = step_key(u);
+  const uint32_t vaddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mv +
+                         (uint32_t)((vk * LPR + (((n & 3) >> 1) ^ piece_swizzle<D>(vk))) * 16 + (n & 1) * 8);
+  auto k_swizzle = [](int key) { return LPR == 8 ? (key >> 1) & 7 : key & 15; };
+  auto v_swizzle = [](int key) { return DT == DT_F32 ? (key >> 2 & 3) * 4 : piece_swizzle<D>(key); };
+  auto store = [&](const u32x4_t(&kr)[NV], u32x4_t(&vr)[NV], bool careful) {
     if (careful) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
@@ -149,21 +164,26 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int r = j * RPI + lane / LPR, seg = lane % LPR;
-      if constexpr (DT == DT_F32) *(u32x4_t*)(mine + r * LD * 4 + seg * 16) = vr[j];
-      else *(u32x4_t*)(mine + (r * LPR + (seg ^ piece_swizzle<D>(r))) * 16) = vr[j];
+      const int r = j * RPI + lr;
+      *(u32x4_t*)(mk + r * RB + (seg ^ k_swizzle(r)) * 16) = kr[j];
+      *(u32x4_t*)(mv + r * RB + (seg ^ v_swizzle(r)) * 16) = vr[j];
     }
+  };
+
+  auto consume = [&](int u, bool careful) {
+    const int k0 = step_key(u);
     float p[KG * 4], top = -INFINITY;
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) {
       f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
+        const u32x4_t kf = *(const u32x4_t*)(mk + (kg * 16 + n) * RB + ((i * 4 + g) ^ k_swizzle(n)) * 16);
         if constexpr (DT == DT_F32) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sacc = mfma_f32(__uint_as_float(kf[kg][i][e]), __uint_as_float(qf[i][e]), sacc);
+          for (int e = 0; e < 4; ++e) sacc = mfma_f32(__uint_as_float(kf[e]), __uint_as_float(qf[i][e]), sacc);
         } else {
-          sacc = mfma16<DT>(kf[kg][i], qf[i], sacc);
+          sacc = mfma16<DT>(kf, qf[i], sacc);
         }
       }
 #pragma unroll
@@ -191,7 +211,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int dt = 0; dt < DTL; ++dt)
-          oacc[dt] = mfma_f32(*(const float*)(mine + ((4 * g + r) * LD + dt * 16 + n) * 4), p[r], oacc[dt]);
+          oacc[dt] = mfma_f32(*(const float*)(mv + (4 * g + r) * RB + ((dt * 4 + (n >> 2)) ^ (g * 4)) * 16 + (n & 3) * 4), p[r], oacc[dt]);
     } else {
       float rest[8];
 #pragma unroll
@@ -237,18 +257,16 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
     for (int dt = 0; dt < DTL; ++dt) oacc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     int u = it.u0 + wave;
     if (u < it.u1) {
-      u32x4_t ka[KG][KS], va[NV], kb[KG][KS], vb[NV];
-      load(ka, va, u);
-      for (; u + 8 < it.u1; u += 8) {
-        load(kb, vb, u + 4);
-        consume(ka, va, u, pass);
-        load(ka, va, u + 8);
-        consume(kb, vb, u + 4, pass);
+      u32x4_t kr[NV], vr[NV];
+      load(place_of(u), kr, vr);
+      for (; u + 4 < it.u1; u += 4) {
+        const Place next = place_of(u + 4);
+        store(kr, vr, pass);
+        load(next, kr, vr);
+        consume(u, pass);
       }
-      const bool two = u + 4 < it.u1;
-      if (two) load(kb, vb, u + 4);
-      consume(ka, va, u, pass);
-      if (two) consume(kb, vb, u + 4, pass);
+      store(kr, vr, pass);
+      consume(u, pass);
     }
     bool fine = true;
 #pragma unroll
@@ -261,7 +279,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
   // the waves' results of a row, in the order of the waves
   l = sum_partner<32>(sum_partner<16>(l));
   __syncthreads();
-  float* my = (float*)mine + n * LD;
+  float* my = (float*)lds[wave] + n * LD;
 #pragma unroll
   for (int dt = 0; dt < DTL; ++dt) *(f32x4_t*)(my + dt * 16 + 4 * g) = oacc[dt];
   if (g == 0) {
@@ -272,7 +290,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedView v, const Page
   const int r = threadIdx.x >> 4, i = threadIdx.x & 15;
   if (it.row0 + r >= rows) return;
   const float* from = (const float*)lds + r * LD;
-  constexpr int W = WAVE_LDS / 4;
+  constexpr int W = 2 * STEP / 4;
   const float mt = fmaxf(fmaxf(from[D], from[W + D]), fmaxf(from[2 * W + D], from[3 * W + D])), ms = mt == -INFINITY ? 0.f : mt;
   float lt = 0.f;
   f32x4_t o[D / 64];
