@@ -106,8 +106,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15;
   const int kvh = blockIdx.x % v.n_kv;
-  const PagedItem it = items[blockIdx.x / v.n_kv];
-  const PagedSeq s = v.seqs[it.seq];
+  const PagedItem& it = items[blockIdx.x / v.n_kv];
+  const PagedSeq s = it.s;
   const int rows = s.fresh * v.group;
   const int row = min(it.row0 + n, rows - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
   const int qpos = s.len - s.fresh + token;                    // sees keys [qlo, qpos] and those below sinks
@@ -126,12 +126,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     uint32_t row[KG];
     int most[KG];
   };
-  auto place_of = [&](int u) {
+  auto place_of = [&](int u, bool first) {
     Place pl;
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) {
       const int p = min(step_key(u) + kg * 16, last16);
-      pl.row[kg] = cache_row(v, s, kvh, p);
+      pl.row[kg] = first ? it.place[2 * wave + kg] + kvh * v.page_size : cache_row(v, s, kvh, p);
       pl.most[kg] = s.len - 1 - p;
     }
     return pl;
@@ -258,9 +258,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     int u = it.u0 + wave;
     if (u < it.u1) {
       u32x4_t kr[NV], vr[NV];
-      load(place_of(u), kr, vr);
+      load(place_of(u, true), kr, vr);
       for (; u + 4 < it.u1; u += 4) {
-        const Place next = place_of(u + 4);
+        const Place next = place_of(u + 4, false);
         store(kr, vr, pass);
         load(next, kr, vr);
         consume(u, pass);
@@ -371,8 +371,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, n = lane & 31;
   const int kvh = blockIdx.x % v.n_kv;
-  const PagedItem it = items[blockIdx.x / v.n_kv];
-  const PagedSeq s = v.seqs[it.seq];
+  const PagedItem& it = items[blockIdx.x / v.n_kv];
+  const PagedSeq s = it.s;
   const int rows = s.fresh * v.group, before = s.len - s.fresh;
   const int row0 = it.row0 + wave * 32;
   const int row = min(row0 + n, rows - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     for (int dt = 0; dt < DTL; ++dt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-    issue(it.u0, cache_row(v, s, kvh, place_of(it.u0)));
+    issue(it.u0, it.place[wave] + kvh * v.page_size);
     uint32_t next = it.u0 + 1 < it.u1 ? cache_row(v, s, kvh, place_of(it.u0 + 1)) : 0;
     for (int u = it.u0; u < it.u1; ++u) {
       copies_barrier<0>(true);                 // step u has landed; every wave is done with step u - 1
@@ -536,39 +536,69 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   }
 }
 
-// Rows whose keys went to several items: block = (rows, key head), 16 threads a row, parts in their order.
-template <int DT, int D>
+// Rows whose keys went to several items.  W waves per row, 4 / W rows per block; D / 4 lanes hold a row, and every group of so many lanes takes
+// its share of the parts, in order; the groups' results are joined in their order.  Few blocks have all the parts of a single long sequence to
+// read: four waves per row then (one row of 64 parts: 32 KB).
+template <int DT, int D, int W>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedView v, const PagedMerge* __restrict__ merges, void* __restrict__ out,
                                                           float* __restrict__ lse) {
+  constexpr int LPR = D / 4, GR = 64 * W / LPR, ROWS = 4 / W;
+  __shared__ __attribute__((aligned(16))) float part[ROWS][GR][D + 4];
   const int kvh = blockIdx.x % v.n_kv;
-  const PagedMerge mg = merges[blockIdx.x / v.n_kv];
-  const PagedSeq s = v.seqs[mg.seq];
-  const int r = threadIdx.x >> 4, i = threadIdx.x & 15;
-  if (mg.row0 + r >= s.fresh * v.group) return;
-  const size_t first = (size_t)mg.part + kvh * mg.tile + r, stride = mg.stride;
+  const PagedMerge& mg = merges[blockIdx.x / v.n_kv];
+  const PagedSeq s = mg.s;
+  const int which = threadIdx.x / (64 * W), r = blockIdx.y * ROWS + which;
+  const int grp = threadIdx.x % (64 * W) / LPR, i = threadIdx.x % LPR * 4;
+  const int rows = min(16, s.fresh * v.group - mg.row0);
+  if (blockIdx.y * ROWS >= rows) return;                       // the whole block
+  const size_t first = (size_t)mg.part + kvh * mg.tile + min(r, rows - 1), stride = mg.stride;
+  float m = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = grp; p0 < mg.parts; p0 += 4 * GR) {
+    float2 ml[4];
+    f32x4_t x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const size_t at = first + (size_t)min(p0 + j * GR, mg.parts - 1) * stride;
+      ml[j] = *(const float2*)(v.pm + at * 2);
+      x[j] = ld4(v.po + at * D + i);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (p0 + j * GR < mg.parts) {
+        const float mn = fmaxf(m, ml[j].x), ms = mn == -INFINITY ? 0.f : mn;
+        const float a = __builtin_amdgcn_exp2f(m - ms), b = __builtin_amdgcn_exp2f(ml[j].x - ms);
+        l = fmaf(b, ml[j].y, a * l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(b, x[j][e], a * o[e]);
+        m = mn;
+      }
+  }
+  float* mine = part[which][grp];
+  *(f32x4_t*)(mine + i) = o;
+  if (i == 0) {
+    mine[D] = m;
+    mine[D + 1] = l;
+  }
+  __syncthreads();
+  if (grp > 0 || r >= rows) return;
   float mt = -INFINITY;
-  for (int p = i; p < mg.parts; p += 16) mt = fmaxf(mt, v.pm[(first + p * stride) * 2]);
-  mt = fmaxf(mt, partner<1>(mt));
-  mt = fmaxf(mt, partner<2>(mt));
-  mt = fmaxf(mt, partner<4>(mt));
-  mt = fmaxf(mt, partner<8>(mt));
+#pragma unroll
+  for (int g = 0; g < GR; ++g) mt = fmaxf(mt, part[which][g][D]);
   const float ms = mt == -INFINITY ? 0.f : mt;
   float lt = 0.f;
-  f32x4_t o[D / 64];
+  o = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int e = 0; e < D / 64; ++e) o[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int p = 0; p < mg.parts; ++p) {
-    const float2 ml = *(const float2*)(v.pm + (first + p * stride) * 2);
-    const float a = __builtin_amdgcn_exp2f(ml.x - ms);
-    lt = fmaf(a, ml.y, lt);
+  for (int g = 0; g < GR; ++g) {
+    const float a = __builtin_amdgcn_exp2f(part[which][g][D] - ms);
+    lt = fmaf(a, part[which][g][D + 1], lt);
+    const f32x4_t x = ld4(&part[which][g][i]);
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) o[e] += a * ld4(v.po + (first + p * stride) * D + i * (D / 16) + e * 4);
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(a, x[e], o[e]);
   }
   const int tk = (mg.row0 + r) / v.group, hd = kvh * v.group + mg.row0 + r - tk * v.group;
   const size_t at = (size_t)(s.first + tk) * v.n_head + hd;
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) stv4<DT>(out, at * D + i * (D / 16) + e * 4, o[e] / lt);
+  stv4<DT>(out, at * D + i, o / lt);
   if (lse && i == 0) lse[at] = mt * kLn2 + logf(lt);
 }
 
@@ -803,7 +833,8 @@ hipError_t paged_append(int dtype, const PagedView& v, const void* k, int64_t ks
 }
 
 hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedItem* tiles, int n_tiles,
-                           const PagedMerge* merges, int n_merges, const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st) {
+                           const PagedMerge* merges, int n_merges, int most_parts, int most_rows,
+                           const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st) {
   with_types(dtype, v.d, [&](auto dt, auto d) {
     constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
     if constexpr (DT != DT_F32)
@@ -811,7 +842,10 @@ hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows,
                                                                               (const char*)vc, out, lse);
     if (n_rows) paged_rows_kernel<DT, D><<<n_rows * v.n_kv, 256, 0, st>>>(v, rows, (const char*)q, qs * element_bytes(DT), (const char*)kc,
                                                                           (const char*)vc, out, lse);
-    if (n_merges) paged_merge_kernel<DT, D><<<n_merges * v.n_kv, 256, 0, st>>>(v, merges, out, lse);
+    if (n_merges) {
+      if (most_parts > 8) paged_merge_kernel<DT, D, 4><<<dim3(n_merges * v.n_kv, most_rows), 256, 0, st>>>(v, merges, out, lse);
+      else paged_merge_kernel<DT, D, 1><<<dim3(n_merges * v.n_kv, (most_rows + 3) / 4), 256, 0, st>>>(v, merges, out, lse);
+    }
   });
   return hipGetLastError();
 }

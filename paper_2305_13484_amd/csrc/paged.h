@@ -19,14 +19,19 @@ struct PagedSeq {
 // A block's work: rows [row0, row0 + tile) of one key head of a sequence over steps [u0, u1) of the keys that some row sees.  Step u is
 // keys step * u .. while u < gap, and step * (u + skip) .. behind: the keys between first tokens and window are left out.
 struct PagedItem {
-  int seq, row0, u0, u1, gap, skip;
+  PagedSeq s;
+  int row0, u0, u1, gap, skip;
   int part;       // first row of its partial result (key head h: h * tile rows further), -1: it has all keys, and writes the output
-  int pad;
+  int pad[2];
+  // rows in the cache, of key head 0, that the block loads first, so that no list has to be read before: of wave w the 16-key groups of its first
+  // step, [2 * w], [2 * w + 1] (streaming kernel), or its group of step u0, [w] (tile kernel)
+  uint32_t place[8];
 };
 // Up to 16 rows whose keys are shared out to `parts` items: partial rows at `part`, `stride` rows from part to part, `tile` from key head to
 // key head.
 struct PagedMerge {
-  int seq, row0, part, stride, parts, tile;
+  PagedSeq s;
+  int row0, part, stride, parts, tile, pad[3];
 };
 
 struct PagedView {     // device memory of a plan, and the shape
@@ -41,8 +46,9 @@ struct PagedView {     // device memory of a plan, and the shape
 };
 
 hipError_t paged_append(int dtype, const PagedView& v, const void* k, int64_t ks, const void* vv, int64_t vs, void* kc, void* vc, hipStream_t st);
+// most_parts, most_rows: of any entry of merges
 hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedItem* tiles, int n_tiles, const PagedMerge* merges, int n_merges,
-                           const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st);
+                           int most_parts, int most_rows, const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st);
 hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t qs, const void* kc, const float* lse, float decay, float* w,
                          int64_t ws, hipStream_t st);
 hipError_t paged_evict(int dtype, const PagedView& v, void* kc, void* vc, const float* w, int64_t ws, int budget, int first, int recent,

@@ -62,11 +62,13 @@ struct Lists {
   size_t pages = 0, places = 0, rows = 0, tiles = 0, merges = 0;      // offsets; the sequences come first
   size_t pm = 0, po = 0, total = 0;                        // partial results, behind the lists
   int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_tiles = 0, n_merges = 0;
+  int most_parts = 0, most_rows = 0;                       // of a merge
   bool shared = false, shared_new = false;                 // a page twice in use; one that new tokens go to
 };
 
-// Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long.
-constexpr int kBlocks[2] = {768, 512};
+// Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long: two of either are at work
+// on a compute unit.
+constexpr int kBlocks[2][2] = {{1024, 2048}, {512, 512}};
 
 int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const int32_t* len, const int32_t* table, int stride, Lists* L) {
   auto bad = [](const std::string& m) { return fail_call(FLOVER_E_INVAL, m); };
@@ -129,7 +131,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   for (int kind = 0; kind < 2; ++kind) {                   // the streaming kernel's work, the tile kernel's
     const int tile = kind ? flk::kTileRows : flk::kRowTile, step = kind ? flk::kTileKeys : flk::row_keys(sh.dtype);
     std::vector<PagedItem> items;
-    int64_t steps = 0;
+    int64_t steps = 0, longest = 0;
     for (int i : order) {
       const int rows_of = new_len[i] * group, before = len[i] - new_len[i];
       if (rows_of == 0 || (sh.dtype != FLOVER_F32 && rows_of > flk::kRowTile) != (kind == 1)) continue;
@@ -142,17 +144,31 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
           gap = (int)std::min<int64_t>(from, ((int64_t)sh.sinks + step - 1) / step);
           skip = from - gap;
         }
-        items.push_back({i, r0, 0, end - skip, gap, skip, -1, 0});
+        items.push_back({seqs[i], r0, 0, end - skip, gap, skip, -1, {0, 0}, {0}});
         steps += end - skip;
+        longest = std::max<int64_t>(longest, end - skip);
       }
     }
-    const int64_t share = std::max<int64_t>(8, (steps * sh.n_kv_head + kBlocks[kind] - 1) / kBlocks[kind]);
+    // The least share of steps, four at least, that makes no more blocks than `most`
+    const int64_t all = steps * sh.n_kv_head;
+    const int64_t most = std::min<int64_t>(kBlocks[kind][1], std::max<int64_t>(kBlocks[kind][0], all / 32));
+    int64_t share = std::max<int64_t>(4, (all + most - 1) / most);
+    for (int64_t low = share, high = std::max<int64_t>(share, longest); low < high; share = high) {
+      const int64_t mid = (low + high) / 2;
+      int64_t blocks = 0;
+      for (const PagedItem& it : items) blocks += (it.u1 + mid - 1) / mid;
+      if (blocks * sh.n_kv_head <= most) high = mid;
+      else low = mid + 1;
+    }
     std::vector<PagedItem>& to = kind ? tiles : rows;
     for (const PagedItem& it : items) {
-      const int parts = it.u1 * 4LL <= share * 5 ? 1 : (int)((it.u1 + share - 1) / share);
-      if (parts > 1)
-        for (int r = 0; r < tile && it.row0 + r < new_len[it.seq] * group; r += 16)
-          merges.push_back({it.seq, it.row0 + r, (int)partial + r, tile * sh.n_kv_head, parts, tile});
+      const int parts = (int)((it.u1 + share - 1) / share), rows_of = it.s.fresh * group;
+      if (parts > 1) {
+        for (int r = 0; r < tile && it.row0 + r < rows_of; r += 16)
+          merges.push_back({it.s, it.row0 + r, (int)partial + r, tile * sh.n_kv_head, parts, tile, {0, 0, 0}});
+        L->most_parts = std::max(L->most_parts, parts);
+        L->most_rows = std::max(L->most_rows, std::min(16, rows_of - it.row0));
+      }
       for (int p = 0; p < parts; ++p) {
         PagedItem x = it;
         x.u0 = (int)((int64_t)it.u1 * p / parts);
@@ -161,6 +177,13 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
         if (parts > 1) {
           x.part = (int)partial;
           partial += (int64_t)tile * sh.n_kv_head;
+        }
+        // where the waves begin
+        for (int w = 0; w < 8; ++w) {
+          const int u = kind ? x.u0 : std::min(x.u0 + w / 2, x.u1 - 1), group16 = kind ? w & 3 : w & 1;
+          const int64_t key = std::min<int64_t>((int64_t)(u < x.gap ? u : u + x.skip) * step + group16 * 16, (x.s.len - 1) & ~15);
+          const int page = (int)(key / sh.page_size);
+          x.place[w] = (uint32_t)pages[x.s.pages + page] * sh.n_kv_head * sh.page_size + (uint32_t)(key - (int64_t)page * sh.page_size);
         }
         to.push_back(x);
       }
@@ -403,7 +426,7 @@ int32_t flover_k_paged_attention(const flover_paged_plan* plan, const void* q, i
     PAGED_TRY(ready(plan, (hipStream_t)stream));
     const Lists& l = plan->lists;
     PAGED_HIP(flk::paged_attention(plan->shape.dtype, plan->view(), (const PagedItem*)(plan->memory + l.rows), l.n_rows,
-                                   (const PagedItem*)(plan->memory + l.tiles), l.n_tiles, (const PagedMerge*)(plan->memory + l.merges), l.n_merges, q, q_stride, kcache, vcache, out, lse,
+                                   (const PagedItem*)(plan->memory + l.tiles), l.n_tiles, (const PagedMerge*)(plan->memory + l.merges), l.n_merges, l.most_parts, l.most_rows, q, q_stride, kcache, vcache, out, lse,
                                    (hipStream_t)stream));
     return FLOVER_OK;
   });
