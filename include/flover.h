@@ -383,7 +383,7 @@ int32_t flover_k_paged_plan_set(flover_paged_plan* plan, int32_t n_seq, const in
 int32_t flover_k_paged_plan_destroy(flover_paged_plan* plan);   /* waits for the plan's last copy; NULL is a no-op */
 
 /* Rows of the new tokens to their places: k, v [device][T] rows of [n_kv_head][head_dim], k_stride / v_stride elements apart
- * (a multiple of 16 bytes; views into a packed q|k|v row are fine), 16-byte aligned.  Refused (INVAL) where two sequences of
+ * (a multiple of 16 bytes, at most 64 MB; views into a packed q|k|v row are fine), 16-byte aligned.  Refused (INVAL) where two sequences of
  * the plan share a page that new tokens go to. */
 int32_t flover_k_paged_append(const flover_paged_plan* plan, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                               void* kcache, void* vcache, void* stream);

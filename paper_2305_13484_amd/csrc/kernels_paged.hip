@@ -604,81 +604,234 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedView v, const Pag
 
 // ---------------------------------------------------------------- weights that the new tokens gave to the cached rows
 
-// grid = (blocks of 256 positions, n_kv, n_seq); a wave holds the K rows of 64 positions and goes through the rows of queries that see any of
-// them, 16 at a time: S[row][key] = Q . K^T leaves a key's scores in one column, so that their exponentials add up in a lane.
+__device__ __forceinline__ void copy_words_to_lds(const char* base, uint32_t off, float* l) {      // 64 lanes x 4 bytes, as copy_to_lds
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, -1, 0x00020000),
+                                           (__attribute__((address_space(3))) void*)l, 4, off, 0, 0, 0);
+}
+// Whether a sequence's weights are the streaming kernel's, or the tile kernel's.
+template <int DT> __device__ __forceinline__ bool few_rows(int rows) { return DT == DT_F32 || rows <= kRowTile; }
+// New tokens [t0, t1) of a sequence see some of keys [k0, k1).
+__device__ __forceinline__ int first_token(const PagedSeq& s, int k0) { return max(0, k0 - (s.len - s.fresh)); }
+__device__ __forceinline__ int end_token(const PagedView& v, const PagedSeq& s, int k0, int k1) {
+  return v.window > 0 && k0 >= v.sinks ? min(s.fresh, k1 - 1 + v.window - (s.len - s.fresh)) : s.fresh;
+}
+// The new weight of position key: rows that the new tokens brought begin with none.
+__device__ __forceinline__ float new_weight(float given, float old, float decay, bool brought) {
+  return decay == 0.f || brought ? given : fmaf(decay, old, given);
+}
+
+// grid = (blocks of kWeighKeys positions, n_kv, n_seq).  Few rows of queries: K streams through as in paged_rows_kernel (a wave takes every
+// fourth step, whole rows to registers, to the wave's piece of LDS, from there as operands) and bounds it.  S[row][key] = Q . K^T leaves a key's
+// scores in one column, so that their exponentials add up in a lane.
+constexpr int kWeighKeys = 512;
 template <int DT, int D>
-__global__ __launch_bounds__(256) void paged_weights_kernel(PagedView v, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc,
-                                                            const float* __restrict__ lse, float decay, float* __restrict__ w, int64_t ws) {
+__global__ __launch_bounds__(256) void paged_weights_rows_kernel(PagedView v, const char* __restrict__ q, int64_t qs,
+                                                                 const char* __restrict__ kc, const float* __restrict__ lse, float decay,
+                                                                 float* __restrict__ w, int64_t ws) {
   constexpr int EB = DT == DT_F32 ? 4 : 2, RB = D * EB, KS = RB / 64;
-  constexpr int KG = DT == DT_F32 ? 2 : 4;                     // 16-key groups held at a time
+  constexpr int KT = DT == DT_F32 ? 16 : 32, KG = KT / 16, LPR = RB / 16, RPI = 64 / LPR, NV = KT / RPI;
+  __shared__ __attribute__((aligned(1024))) char lds[4][KT * RB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15, kvh = blockIdx.y;
   const PagedSeq s = v.seqs[blockIdx.z];
+  if (!few_rows<DT>(s.fresh * v.group)) return;
   const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
+  const int end = min(s.len, (int)(blockIdx.x + 1) * kWeighKeys);
+  int k0 = blockIdx.x * kWeighKeys + wave * KT;
+  if (k0 >= end) return;
   const float c = v.scale * kLog2e;
-  for (int half = 0; half < 4 / KG; ++half) {
-    const int k0 = blockIdx.x * 256 + wave * 64 + half * KG * 16;
-    if (k0 >= s.len) return;
-    const int k1 = min(k0 + KG * 16, s.len);                   // keys [k0, k1)
-    // new tokens that see some of them: [t0, t1)
-    const int t0 = max(0, k0 - before);
-    const int t1 = v.window > 0 && k0 >= v.sinks ? min(s.fresh, k1 - 1 + v.window - before) : s.fresh;
+  char* mk = lds[wave];
+  auto k_swizzle = [](int key) { return LPR == 8 ? (key >> 1) & 7 : key & 15; };
+  u32x4_t kr[NV];
+  const int lr = lane / LPR, seg = lane % LPR;
+  auto load = [&](int k) {
+    uint32_t row[KG];
+#pragma unroll
+    for (int kg = 0; kg < KG; ++kg) row[kg] = cache_row(v, s, kvh, min(k + kg * 16, last16));
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      constexpr int G = 16 / RPI;
+      const int most = s.len - 1 - min(k + j / G * 16, last16);
+      kr[j] = load_rows<DT>(kc + (size_t)(row[j / G] + min(j % G * RPI + lr, most)) * RB + seg * 16);
+    }
+  };
+  u32x4_t qf[KS];
+  float base[4];                                               // of rows r0 + 4g + r: lse in base 2, and the position
+  int at[4];
+  auto queries = [&](int r0, int r1) {
+    const int row = min(r0 + n, r1 - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
+    const char* qr = q + (s.first + token) * qs + (size_t)head * RB + g * 16;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) qf[i] = *(const u32x4_t*)(qr + i * 64);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int rr = min(r0 + 4 * g + r, r1 - 1), tk = rr / v.group;
+      base[r] = lse[(size_t)(s.first + tk) * v.n_head + kvh * v.group + rr - tk * v.group] * kLog2e;
+      at[r] = r0 + 4 * g + r < r1 ? before + tk : -1;          // -1: no such row
+    }
+  };
+  const bool one = s.fresh * v.group <= kRowTile;              // all rows of queries at once: they stay in registers
+  load(k0);
+  if (one && s.fresh > 0) queries(0, s.fresh * v.group);
+  for (; k0 < end; k0 += 4 * KT) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int r = j * RPI + lr;
+      *(u32x4_t*)(mk + r * RB + (seg ^ k_swizzle(r)) * 16) = kr[j];
+    }
+    // the lane that holds a key's sum at the end: group kg of the lanes key group kg
+    const int mine = k0 + g * 16 + n;
+    float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + mine;
+    const bool writes = g < KG && mine < s.len, brought = mine >= before;
+    const float old = writes && decay != 0.f && !brought ? *to : 0.f;
+    if (k0 + 4 * KT < end) load(k0 + 4 * KT);
+    const int k1 = min(k0 + KT, s.len), t0 = first_token(s, k0), t1 = end_token(v, s, k0, k1);
     float sum[KG];
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) sum[kg] = 0.f;
-    if (t0 < t1) {
-      u32x4_t kf[KG][KS];
+    for (int r0 = one ? 0 : t0 * v.group; t0 < t1 && r0 < t1 * v.group; r0 += 16) {
+      if (!one) queries(r0, t1 * v.group);
 #pragma unroll
       for (int kg = 0; kg < KG; ++kg) {
-        const int p = min(k0 + kg * 16, last16);
-        const char* kp = kc + (size_t)(cache_row(v, s, kvh, p) + min(n, s.len - 1 - p)) * RB + g * 16;
+        f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < KS; ++i) kf[kg][i] = *(const u32x4_t*)(kp + i * 64);
-      }
-      const int r1 = t1 * v.group;
-      for (int r0 = t0 * v.group; r0 < r1; r0 += 16) {
-        const int row = min(r0 + n, r1 - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
-        const char* qr = q + (s.first + token) * qs + (size_t)head * RB + g * 16;
-        u32x4_t qf[KS];
+        for (int i = 0; i < KS; ++i) {
+          const u32x4_t kf = *(const u32x4_t*)(mk + (kg * 16 + n) * RB + ((i * 4 + g) ^ k_swizzle(n)) * 16);
+          if constexpr (DT == DT_F32) {
 #pragma unroll
-        for (int i = 0; i < KS; ++i) qf[i] = *(const u32x4_t*)(qr + i * 64);
-        float base[4];                                         // of rows r0 + 4g + r: lse in base 2, and the position
-        int at[4];
+            for (int e = 0; e < 4; ++e) sacc = mfma_f32(__uint_as_float(qf[i][e]), __uint_as_float(kf[e]), sacc);
+          } else {
+            sacc = mfma16<DT>(qf[i], kf, sacc);
+          }
+        }
+        const int key = k0 + kg * 16 + n;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int rr = min(r0 + 4 * g + r, r1 - 1), tk = rr / v.group;
-          base[r] = lse[(size_t)(s.first + tk) * v.n_head + kvh * v.group + rr - tk * v.group] * kLog2e;
-          at[r] = r0 + 4 * g + r < r1 ? before + tk : -1;      // -1: no such row
-        }
-#pragma unroll
-        for (int kg = 0; kg < KG; ++kg) {
-          f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < KS; ++i) {
-            if constexpr (DT == DT_F32) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) sacc = mfma_f32(__uint_as_float(qf[i][e]), __uint_as_float(kf[kg][i][e]), sacc);
-            } else {
-              sacc = mfma16<DT>(qf[i], kf[kg][i], sacc);
-            }
-          }
-          const int key = k0 + kg * 16 + n;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const bool seen = key <= at[r] && (v.window <= 0 || key > at[r] - v.window || key < v.sinks);
-            sum[kg] += seen ? __builtin_amdgcn_exp2f(fmaf(sacc[r], c, -base[r])) : 0.f;
-          }
+          const bool seen = key <= at[r] && (v.window <= 0 || key > at[r] - v.window || key < v.sinks);
+          sum[kg] += seen ? __builtin_amdgcn_exp2f(fmaf(sacc[r], c, -base[r])) : 0.f;
         }
       }
     }
+    float t = 0.f;
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) {
-      const float t = sum_partner<32>(sum_partner<16>(sum[kg]));
-      const int key = k0 + kg * 16 + n;
-      if (g == kg % 4 && key < s.len) {
-        float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + key;
-        *to = decay == 0.f || key >= before ? t : fmaf(decay, *to, t);
+      const float x = sum_partner<32>(sum_partner<16>(sum[kg]));
+      t = g == kg ? x : t;
+    }
+    if (writes) *to = new_weight(t, old, decay, brought);
+  }
+}
+
+// Many rows of queries, 16-bit types; grid = (blocks of 4 * 32 * KW positions, n_kv, n_seq).  A wave holds the K rows of 32 * KW positions as
+// operands and goes through the rows that see any of the block's, 32 at a time, which come to LDS by asynchronous copies, four steps in a ring, for all
+// waves.  S[row][key] as above: a lane adds up 16 rows of its key.  An exponential takes 16 cycles of a wave's vector unit and a product of its
+// 32 x 32 x 16 scores 32 of the matrix unit, eight for d = 128: the products bound it.
+constexpr int kWeighRing = 4;
+template <int DT, int D, int KW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_weights_tile_kernel(
+    PagedView v, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc, const float* __restrict__ lse, float decay,
+    float* __restrict__ w, int64_t ws) {
+  constexpr int RB = D * 2, KS = D / 16, SEG = D / 8, RPC = 64 / SEG, NC = 8 / RPC;      // copies of a wave's 8 rows of a step
+  __shared__ __attribute__((aligned(1024))) char rows_lds[kWeighRing][32 * RB];
+  __shared__ __attribute__((aligned(1024))) float lse_lds[kWeighRing][4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, n = lane & 31, kvh = blockIdx.y;
+  const PagedSeq s = v.seqs[blockIdx.z];
+  if (few_rows<DT>(s.fresh * v.group)) return;
+  constexpr int KEYS = 32 * KW;
+  const int kb0 = blockIdx.x * 4 * KEYS;
+  if (kb0 >= s.len) return;
+  const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
+  const int k0 = kb0 + wave * KEYS;
+  // rows that see some key of the block, of the wave
+  const int kb1 = min(kb0 + 4 * KEYS, s.len), k1 = min(k0 + KEYS, s.len);
+  const int b0 = first_token(s, kb0) * v.group, b1 = end_token(v, s, kb0, kb1) * v.group;
+  const int t0 = first_token(s, k0), t1 = k0 < s.len ? end_token(v, s, k0, k1) : 0;
+  const float c = v.scale * kLog2e;
+
+  u32x4_t kf[KW][KS];
+#pragma unroll
+  for (int x = 0; x < KW; ++x) {
+    const int p = min(k0 + x * 32 + (n & 16), last16);
+    const int pl = __builtin_amdgcn_readlane(p, 0), ph = __builtin_amdgcn_readlane(p, 16);
+    const uint32_t rl = cache_row(v, s, kvh, pl), rh = cache_row(v, s, kvh, ph);
+    const char* kr = kc + (size_t)((n & 16 ? rh : rl) + min(n & 15, s.len - 1 - p)) * RB + h * 16;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) kf[x][i] = *(const u32x4_t*)(kr + i * 32);
+  }
+  auto swizzle = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
+  auto issue = [&](int u) {
+    const int r0 = b0 + u * 32, ta = r0 / v.group;              // the step's first token: offsets from there fit 32 bits
+    const char* qb = q + (s.first + ta) * qs + (size_t)kvh * v.group * RB;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int r = wave * 8 + j * RPC + lane / SEG, row = min(r0 + r, b1 - 1), token = row / v.group;
+      copy_to_lds(qb, (uint32_t)((token - ta) * (int)qs + (row - token * v.group) * RB) + ((lane % SEG) ^ swizzle(r)) * 16,
+                  (u32x4_t*)(rows_lds[u % kWeighRing] + (wave * 8 + j * RPC) * RB));
+    }
+    const int row = min(r0 + n, b1 - 1), token = row / v.group;
+    copy_words_to_lds((const char*)(lse + (size_t)(s.first + ta) * v.n_head + kvh * v.group),
+                      (uint32_t)(((token - ta) * v.n_head + row - token * v.group) * 4), lse_lds[u % kWeighRing][wave]);
+  };
+  const int steps = b1 > b0 ? (b1 - b0 + 31) / 32 : 0;
+  float sum[KW];
+#pragma unroll
+  for (int x = 0; x < KW; ++x) sum[x] = 0.f;
+#pragma unroll
+  for (int u = 0; u < kWeighRing - 1; ++u)
+    if (u < steps) issue(u);
+  for (int u = 0; u < steps; ++u) {
+    copies_barrier<(NC + 1) * (kWeighRing - 2)>(u + kWeighRing - 2 >= steps);
+    if (u + kWeighRing - 1 < steps) issue(u + kWeighRing - 1);
+    const int r0 = b0 + u * 32, ta = r0 / v.group, tb = min(r0 + 31, b1 - 1) / v.group;
+    if (tb < t0 || ta >= t1) continue;
+    const char* ql = rows_lds[u % kWeighRing] + n * RB;
+    const float* ll = lse_lds[u % kWeighRing][wave];
+    f32x16_t sacc[KW];
+#pragma unroll
+    for (int x = 0; x < KW; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sacc[x][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4_t qf = *(const u32x4_t*)(ql + ((ks * 2 + h) ^ swizzle(n)) * 16);
+#pragma unroll
+      for (int x = 0; x < KW; ++x) sacc[x] = mfma32<DT>(qf, kf[x][ks], sacc[x]);
+    }
+    float base[16];
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const f32x4_t b = ld4(ll + 2 * i + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) base[i + e] = b[e] * kLog2e;
+    }
+    const bool full = k0 + KEYS - 1 <= before + ta && r0 + 32 <= b1 &&
+                      (v.window <= 0 || k0 > before + tb - v.window || k0 + KEYS <= v.sinks);
+    if (full) {
+#pragma unroll
+      for (int x = 0; x < KW; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[x] += __builtin_amdgcn_exp2f(fmaf(sacc[x][i], c, -base[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = r0 + (i & 3) + 8 * (i >> 2) + 4 * h, pos = row < b1 ? before + row / v.group : -1;
+#pragma unroll
+        for (int x = 0; x < KW; ++x) {
+          const int key = k0 + x * 32 + n;
+          const bool seen = key <= pos && (v.window <= 0 || key > pos - v.window || key < v.sinks);
+          sum[x] += seen ? __builtin_amdgcn_exp2f(fmaf(sacc[x][i], c, -base[i])) : 0.f;
+        }
       }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < KW; ++x) {
+    const float t = sum_partner<32>(sum[x]);
+    const int key = k0 + x * 32 + n;
+    if (h == 0 && key < s.len) {
+      float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + key;
+      *to = new_weight(t, decay != 0.f && key < before ? *to : 0.f, decay, key >= before);
     }
   }
 }
@@ -851,11 +1004,15 @@ hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows,
 }
 
 hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t qs, const void* kc, const float* lse, float decay, float* w,
-                         int64_t ws, hipStream_t st) {
+                         int64_t ws, bool few, bool many, hipStream_t st) {
   with_types(dtype, v.d, [&](auto dt, auto d) {
     constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
-    paged_weights_kernel<DT, D><<<dim3((v.longest + 255) / 256, v.n_kv, v.n_seq), 256, 0, st>>>(
-        v, (const char*)q, qs * element_bytes(DT), (const char*)kc, lse, decay, w, ws);
+    const int64_t qb = qs * element_bytes(DT);
+    if (few) paged_weights_rows_kernel<DT, D><<<dim3((v.longest + kWeighKeys - 1) / kWeighKeys, v.n_kv, v.n_seq), 256, 0, st>>>(
+        v, (const char*)q, qb, (const char*)kc, lse, decay, w, ws);
+    if constexpr (DT != DT_F32)
+      if (many) paged_weights_tile_kernel<DT, D, 1><<<dim3((v.longest + 127) / 128, v.n_kv, v.n_seq), 256, 0, st>>>(
+          v, (const char*)q, qb, (const char*)kc, lse, decay, w, ws);
   });
   return hipGetLastError();
 }

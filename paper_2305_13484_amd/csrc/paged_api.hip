@@ -63,6 +63,7 @@ struct Lists {
   size_t pm = 0, po = 0, total = 0;                        // partial results, behind the lists
   int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_tiles = 0, n_merges = 0;
   int most_parts = 0, most_rows = 0;                       // of a merge
+  bool few = false, many = false;                          // sequences of up to 16 rows per key head (of fp32: all), of more
   bool shared = false, shared_new = false;                 // a page twice in use; one that new tokens go to
 };
 
@@ -104,6 +105,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   for (int i = 0; i < n_seq; ++i) {
     const int need = (len[i] + sh.page_size - 1) / sh.page_size, fresh = len[i] - new_len[i];
     seqs[i] = {first, new_len[i], len[i], (int)pages.size()};
+    (sh.dtype == FLOVER_F32 || new_len[i] * group <= flk::kRowTile ? L->few : L->many) = true;
     for (int p = 0; p < need; ++p) {
       const int page = table[(size_t)i * stride + p];
       const bool written = new_len[i] > 0 && (int64_t)(p + 1) * sh.page_size > fresh;
@@ -283,8 +285,8 @@ int ready(const flover_paged_plan* p, hipStream_t st) {
 // Checks of a row tensor [tokens] of `width` elements, `stride` apart.
 int check_rows(const flover_paged_plan* p, const void* x, int64_t stride, int64_t width, const char* name) {
   if (!x) return fail_call(FLOVER_E_INVAL, std::string("null ") + name);
-  if (!aligned16(x) || stride < width || stride % (16 / esize(p->shape.dtype)))
-    return fail_call(FLOVER_E_INVAL, std::string(name) + ": rows on 16 bytes, a stride of at least the row");
+  if (!aligned16(x) || stride < width || stride % (16 / esize(p->shape.dtype)) || stride > (int64_t)(1 << 26) / esize(p->shape.dtype))
+    return fail_call(FLOVER_E_INVAL, std::string(name) + ": rows on 16 bytes, a stride of at least the row and at most 64 MB");
   return FLOVER_OK;
 }
 int check_plan(const flover_paged_plan* p) {
@@ -451,7 +453,8 @@ int32_t flover_k_paged_weights(const flover_paged_plan* plan, const void* q, int
         (l.tokens && overlap(weights, nw, lse, (size_t)l.tokens * plan->shape.n_head * 4)))
       return fail_call(FLOVER_E_INVAL, "the weights share memory with what is read");
     PAGED_TRY(ready(plan, (hipStream_t)stream));
-    PAGED_HIP(flk::paged_weights(plan->shape.dtype, plan->view(), q, q_stride, kcache, lse, decay, weights, weight_stride, (hipStream_t)stream));
+    PAGED_HIP(flk::paged_weights(plan->shape.dtype, plan->view(), q, q_stride, kcache, lse, decay, weights, weight_stride, l.few,
+                                 l.many, (hipStream_t)stream));
     return FLOVER_OK;
   });
 }
