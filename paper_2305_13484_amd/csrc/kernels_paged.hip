@@ -11,12 +11,25 @@ namespace flk {
 
 namespace {
 
+// Lambdas whose captures have to stay in registers.
+#define INLINED __attribute__((always_inline))
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// What a plan's lists hold is constant while a kernel runs: scalar loads, which no vector load or copy is waited for with.
+template <class T> __device__ __forceinline__ T uniform_load(const T* p) {
+  struct Words {
+    int w[sizeof(T) / 4];
+  } x;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) x.w[i] = ((const __attribute__((address_space(4))) int*)(uintptr_t)p)[i];
+  return __builtin_bit_cast(T, x);
+}
 
 // Row of position pos (uniform in a wave) of a sequence in the cache of one key head.
 __device__ __forceinline__ uint32_t cache_row(const PagedView& v, const PagedSeq& s, int kvh, int pos) {
-  const int page = v.page_shift >= 0 ? pos >> v.page_shift : pos / v.page_size;
-  return ((uint32_t)v.pages[s.pages + page] * v.n_kv + kvh) * v.page_size + (uint32_t)(pos - page * v.page_size);
+  const int page = quotient(pos, v.by_page);
+  return ((uint32_t)uniform_load(v.pages + s.pages + page) * v.n_kv + kvh) * v.page_size + (uint32_t)(pos - page * v.page_size);
 }
 
 // ---------------------------------------------------------------- rows of new tokens
@@ -106,10 +119,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15;
   const int kvh = blockIdx.x % v.n_kv;
-  const PagedItem& it = items[blockIdx.x / v.n_kv];
+  const PagedItem* ip = items + blockIdx.x / v.n_kv;
+  const PagedItem it = uniform_load(ip);
   const PagedSeq s = it.s;
   const int rows = s.fresh * v.group;
-  const int row = min(it.row0 + n, rows - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
+  const int row = min(it.row0 + n, rows - 1), token = quotient(row, v.by_group), head = kvh * v.group + row - token * v.group;
   const int qpos = s.len - s.fresh + token;                    // sees keys [qlo, qpos] and those below sinks
   const int qlo = v.window > 0 ? qpos - v.window + 1 : 0;
   const int last16 = (s.len - 1) & ~15;
@@ -126,18 +140,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     uint32_t row[KG];
     int most[KG];
   };
-  auto place_of = [&](int u, bool first) {
+  auto place_of = [&](int u, bool first) INLINED {
     Place pl;
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) {
       const int p = min(step_key(u) + kg * 16, last16);
-      pl.row[kg] = first ? it.place[2 * wave + kg] + kvh * v.page_size : cache_row(v, s, kvh, p);
+      pl.row[kg] = first ? uniform_load(&ip->place[2 * wave + kg]) + kvh * v.page_size : cache_row(v, s, kvh, p);
       pl.most[kg] = s.len - 1 - p;
     }
     return pl;
   };
   const int lr = lane / LPR, seg = lane % LPR;
-  auto load = [&](const Place& pl, u32x4_t(&kr)[NV], u32x4_t(&vr)[NV]) {
+  auto load = [&](const Place& pl, u32x4_t(&kr)[NV], u32x4_t(&vr)[NV]) INLINED {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       constexpr int G = 16 / RPI;             // loads of a group
@@ -155,8 +169,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
                          (uint32_t)((vk * LPR + (((n & 3) >> 1) ^ piece_swizzle<D>(vk))) * 16 + (n & 1) * 8);
   auto k_swizzle = [](int key) { return LPR == 8 ? (key >> 1) & 7 : key & 15; };
   auto v_swizzle = [](int key) { return DT == DT_F32 ? (key >> 2 & 3) * 4 : piece_swizzle<D>(key); };
-  auto store = [&](const u32x4_t(&kr)[NV], u32x4_t(&vr)[NV], bool careful) {
-    if (careful) {
+  auto store = [&](const u32x4_t(&kr)[NV], u32x4_t(&vr)[NV], auto careful) INLINED {
+    if constexpr (decltype(careful)::value) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -170,7 +184,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     }
   };
 
-  auto consume = [&](int u, bool careful) {
+  auto consume = [&](int u, auto careful) INLINED {
     const int k0 = step_key(u);
     float p[KG * 4], top = -INFINITY;
 #pragma unroll
@@ -189,7 +203,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int key = k0 + kg * 16 + 4 * g + r;
-        const bool seen = key <= qpos && (key >= qlo || key < v.sinks);
+        const bool seen = (key <= qpos) & ((key >= qlo) | (key < v.sinks));
         p[kg * 4 + r] = seen ? sacc[r] * c : -INFINITY;
         top = fmaxf(top, p[kg * 4 + r]);
       }
@@ -233,24 +247,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
         }
       }
     }
-    if (careful) {
+    if constexpr (decltype(careful)::value) {
       for (int j = 0; j < KT; ++j) {
         const int key = k0 + j;
         if (key >= s.len) break;
         const uint32_t r = cache_row(v, s, kvh, key & ~15) + (key & 15);
-        const bool seen = key <= qpos && (key >= qlo || key < v.sinks);
+        const bool seen = (key <= qpos) & ((key >= qlo) | (key < v.sinks));
 #pragma unroll
         for (int dt = 0; dt < DTL; ++dt) {
           const f32x4_t x = ldv4<DT>(vc, (size_t)r * D + dt * 16 + 4 * g);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (seen && !is_finite(x[e])) oacc[dt][e] += x[e];
+          for (int e = 0; e < 4; ++e) oacc[dt][e] += (seen & !is_finite(x[e])) ? x[e] : 0.f;
         }
       }
     }
   };
 
-  for (int pass = 0; pass < 2; ++pass) {
+  auto all_keys = [&](auto careful) INLINED {
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
@@ -261,20 +274,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       load(place_of(u, true), kr, vr);
       for (; u + 4 < it.u1; u += 4) {
         const Place next = place_of(u + 4, false);
-        store(kr, vr, pass);
+        store(kr, vr, careful);
         load(next, kr, vr);
-        consume(u, pass);
+        consume(u, careful);
       }
-      store(kr, vr, pass);
-      consume(u, pass);
+      store(kr, vr, careful);
+      consume(u, careful);
     }
     bool fine = true;
 #pragma unroll
     for (int dt = 0; dt < DTL; ++dt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) fine = fine && is_finite(oacc[dt][e]);
-    if (__all(fine)) break;
-  }
+      for (int e = 0; e < 4; ++e) fine &= is_finite(oacc[dt][e]);
+    return fine;
+  };
+  if (!__all(all_keys(std::false_type{}))) all_keys(std::true_type{});
 
   // the waves' results of a row, in the order of the waves
   l = sum_partner<32>(sum_partner<16>(l));
@@ -303,7 +317,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) o[e] += a * ld4(from + w * W + i * (D / 16) + e * 4);
   }
-  const int tk = (it.row0 + r) / v.group, hd = kvh * v.group + it.row0 + r - tk * v.group;
+  const int tk = quotient(it.row0 + r, v.by_group), hd = kvh * v.group + it.row0 + r - tk * v.group;
   if (it.part < 0) {
     const size_t at = (size_t)(s.first + tk) * v.n_head + hd;
 #pragma unroll
@@ -351,6 +365,24 @@ template <int HI> __device__ __forceinline__ void read_keys_of_32d(const uint32_
 }
 template <int HI> __device__ __forceinline__ void read_keys_of_32d(const uint32_t (&a)[4], u32x4_t (&v)[4]) { read_keys_of_d<HI>(a, v); }
 
+// 16 bytes of LDS from each of N addresses, OFF bytes further, with their wait: at an LDS read of its own the compiler waits for every
+// asynchronous copy in flight.
+template <int OFF> __device__ __forceinline__ void read_pieces(const uint32_t (&a)[4], u32x4_t (&v)[4]) {
+  asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\tds_read_b128 %2, %6 offset:%8\n\t"
+               "ds_read_b128 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(OFF)
+               : "memory");
+}
+template <int OFF> __device__ __forceinline__ void read_pieces(const uint32_t (&a)[8], u32x4_t (&v)[8]) {
+  asm volatile("ds_read_b128 %0, %8 offset:%16\n\tds_read_b128 %1, %9 offset:%16\n\tds_read_b128 %2, %10 offset:%16\n\t"
+               "ds_read_b128 %3, %11 offset:%16\n\tds_read_b128 %4, %12 offset:%16\n\tds_read_b128 %5, %13 offset:%16\n\t"
+               "ds_read_b128 %6, %14 offset:%16\n\tds_read_b128 %7, %15 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]), "n"(OFF)
+               : "memory");
+}
+
 // One item of 128 query rows of a key head, 32 per wave; the block's waves share the keys, 64 at a time, the next 64 rows of K and V on their way
 // to LDS (asynchronous copies, two buffers) while the present ones are worked on.  16-bit types.
 //   scores   S^T[key][row] = K . Q^T in tiles of 32 x 32, so that a row's scores lie in two lanes;
@@ -371,14 +403,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, n = lane & 31;
   const int kvh = blockIdx.x % v.n_kv;
-  const PagedItem& it = items[blockIdx.x / v.n_kv];
+  const PagedItem* ip = items + blockIdx.x / v.n_kv;
+  const PagedItem it = uniform_load(ip);
   const PagedSeq s = it.s;
   const int rows = s.fresh * v.group, before = s.len - s.fresh;
   const int row0 = it.row0 + wave * 32;
-  const int row = min(row0 + n, rows - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
+  const int row = min(row0 + n, rows - 1), token = quotient(row, v.by_group), head = kvh * v.group + row - token * v.group;
   const int qpos = before + token, qlo = v.window > 0 ? qpos - v.window + 1 : 0;
   // positions of the wave's rows: [p0, p1]
-  const int p0 = before + min(row0, rows - 1) / v.group, p1 = row0 < rows ? before + min(row0 + 31, rows - 1) / v.group : -1;
+  const int p0 = before + quotient(min(row0, rows - 1), v.by_group), p1 = row0 < rows ? before + quotient(min(row0 + 31, rows - 1), v.by_group) : -1;
   const int last16 = (s.len - 1) & ~15;
   u32x4_t qf[KS];
   const char* qr = q + (s.first + token) * qs + (size_t)head * RB + h * 16;
@@ -388,9 +421,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 
   auto step_key = [&](int u) { return (u < it.gap ? u : u + it.skip) * kTileKeys; };
   // a wave copies rows 16 * wave .. + 15 of a step; rows behind the last repeat it (hidden below)
-  auto place_of = [&](int u) { return min(step_key(u) + wave * 16, last16); };
+  auto place_of = [&](int u) INLINED { return min(step_key(u) + wave * 16, last16); };
   auto k_swizzle = [](int key) { return D == 128 ? key & 15 : (key >> 1) & 7; };
-  auto issue = [&](int u, uint32_t r0) {
+  auto issue = [&](int u, uint32_t r0) INLINED {
     char(*buf)[BUF] = lds[(u - it.u0) & 1];
     const int most = s.len - 1 - place_of(u);
     const char *kb = kc + (size_t)r0 * RB, *vb = vc + (size_t)r0 * RB;
@@ -404,39 +437,52 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0];
   // this lane's 8 bytes of V for the first operand: key 4h + i / 4, d 16 * (second 16 lanes) + 4 * (i % 4), i = lane % 16
   const int vk = 4 * h + ((lane & 15) >> 2), vp = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const uint32_t kaddr = lds_at + (uint32_t)(n * RB + (h ^ k_swizzle(n)) * 16);
   const uint32_t vaddr = lds_at + BUF + (uint32_t)(vk * RB + (vp ^ piece_swizzle<D>(vk)) * 16 + (lane & 1) * 8);
 
   f32x16_t oacc[DTL];
   float m, l;                                 // the running maximum (of unscaled scores), this lane's share of the sum
-  auto consume = [&](int u, bool careful) {
+  auto consume = [&](int u, auto careful_) INLINED {
+    constexpr bool careful = decltype(careful_)::value;
     const int k0 = step_key(u), b = (u - it.u0) & 1;
     if (k0 > p1) return;                      // none of the wave's rows sees these keys
-    const bool full = k0 + kTileKeys - 1 <= p0 && (v.window <= 0 || k0 > p1 - v.window || k0 + kTileKeys <= v.sinks) && !careful;
+    const bool full = k0 + kTileKeys - 1 <= p0 && (v.window <= 0 || k0 > p1 - v.window || k0 + kTileKeys <= v.sinks);
     f32x16_t sacc[2];
-    const char* kl = lds[b][0];
+    uint32_t ka[KS];
+    u32x4_t kf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) ka[ks] = (kaddr + b * (2 * BUF)) ^ (ks * 32);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const char* kr = kl + (kt * 32 + n) * RB;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sacc[kt][i] = 0.f;
+      if (kt == 0) read_pieces<0>(ka, kf);
+      else read_pieces<32 * RB>(ka, kf);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        sacc[kt] = mfma32<DT>(*(const u32x4_t*)(kr + (((ks * 2 + h) ^ k_swizzle(n)) * 16)), qf[ks], sacc[kt]);
+      for (int ks = 0; ks < KS; ++ks) sacc[kt] = mfma32<DT>(kf[ks], qf[ks], sacc[kt]);
     }
-    if (!full) {
+    u32x4_t va[4][DTL];                       // on their way while the products are worked on
+#pragma unroll
+    for (int st = 0; st < 4; ++st) {
+      uint32_t at[DTL];
+#pragma unroll
+      for (int dt = 0; dt < DTL; ++dt) at[dt] = (vaddr + b * (2 * BUF) + st * 16 * RB) ^ (dt * 64);
+      read_keys_of_32d<8 * RB>(at, va[st]);
+    }
+    if (careful || !full) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = k0 + kt * 32 + (i & 3) + 8 * (i >> 2) + 4 * h;
-          if (!(key <= qpos && (key >= qlo || key < v.sinks))) sacc[kt][i] = -INFINITY;
+          sacc[kt][i] = ((key <= qpos) & ((key >= qlo) | (key < v.sinks))) ? sacc[kt][i] : -INFINITY;
         }
     }
     float top = sacc[0][0];
 #pragma unroll
     for (int i = 1; i < 32; ++i) top = fmaxf(top, sacc[i >> 4][i & 15]);
     top = max_partner<32>(top);
-    if (__any((top - m) * c > 8.f || (m == -INFINITY && top > m))) {
+    if (__any((top - m) * c > 8.f)) {          // (a first maximum passes minus infinity by infinity)
       const float mn = fmaxf(m, top);
       const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * c);
       m = mn;
@@ -456,65 +502,59 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       u32x4_t pb;
 #pragma unroll
       for (int e = 0; e < 4; ++e) pb[e] = round_pair<DT>(sacc[st >> 1][(st & 1) * 8 + 2 * e], sacc[st >> 1][(st & 1) * 8 + 2 * e + 1]);
-      uint32_t at[DTL];
-      u32x4_t va[DTL];
-#pragma unroll
-      for (int dt = 0; dt < DTL; ++dt) at[dt] = (vaddr + b * (2 * BUF) + st * 16 * RB) ^ (dt * 64);
-      read_keys_of_32d<8 * RB>(at, va);
 #pragma unroll
       for (int dt = 0; dt < DTL; ++dt) {
-        if (careful) {
+        if constexpr (careful) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) va[dt][e] = finite_only<DT>(va[dt][e]);
+          for (int e = 0; e < 4; ++e) va[st][dt][e] = finite_only<DT>(va[st][dt][e]);
         }
-        oacc[dt] = mfma32<DT>(va[dt], pb, oacc[dt]);
+        oacc[dt] = mfma32<DT>(va[st][dt], pb, oacc[dt]);
       }
     }
-    if (careful) {
+    if constexpr (careful) {
       for (int j = 0; j < kTileKeys; ++j) {
         const int key = k0 + j;
         if (key >= s.len) break;
         const uint32_t r = cache_row(v, s, kvh, key & ~15) + (key & 15);
-        const bool seen = key <= qpos && (key >= qlo || key < v.sinks);
+        const bool seen = (key <= qpos) & ((key >= qlo) | (key < v.sinks));
 #pragma unroll
         for (int dt = 0; dt < DTL; ++dt)
 #pragma unroll
           for (int i = 0; i < 16; i += 4) {
             const f32x4_t x = ldv4<DT>(vc, (size_t)r * D + dt * 32 + 2 * i + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (seen && !is_finite(x[e])) oacc[dt][i + e] += x[e];
+            for (int e = 0; e < 4; ++e) oacc[dt][i + e] += (seen & !is_finite(x[e])) ? x[e] : 0.f;
           }
       }
     }
   };
-
-  for (int pass = 0; pass < 2; ++pass) {
+  auto all_keys = [&](auto careful) INLINED {
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DTL; ++dt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-    issue(it.u0, it.place[wave] + kvh * v.page_size);
+    issue(it.u0, uniform_load(&ip->place[wave]) + kvh * v.page_size);
     uint32_t next = it.u0 + 1 < it.u1 ? cache_row(v, s, kvh, place_of(it.u0 + 1)) : 0;
     for (int u = it.u0; u < it.u1; ++u) {
       copies_barrier<0>(true);                 // step u has landed; every wave is done with step u - 1
       if (u + 1 < it.u1) issue(u + 1, next);
       if (u + 2 < it.u1) next = cache_row(v, s, kvh, place_of(u + 2));
-      consume(u, pass);
+      consume(u, careful);
     }
     bool fine = true;
 #pragma unroll
     for (int dt = 0; dt < DTL; ++dt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) fine = fine && is_finite(oacc[dt][i]);
-    if (!__syncthreads_or(!fine)) break;       // (and behind it the buffers are free)
-  }
+      for (int i = 0; i < 16; ++i) fine &= is_finite(oacc[dt][i]);
+    return fine;
+  };
+  if (__syncthreads_or(!all_keys(std::false_type{}))) all_keys(std::true_type{});      // (behind the barrier the buffers are free)
 
   l = sum_partner<32>(l);
   if (row0 + n >= rows) return;
-  const int tk = (row0 + n) / v.group;
+  const int tk = quotient(row0 + n, v.by_group);
   if (it.part < 0) {
     const size_t at = (size_t)(s.first + tk) * v.n_head + kvh * v.group + row0 + n - tk * v.group;
     const float inv = 1.f / l;
@@ -545,7 +585,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedView v, const Pag
   constexpr int LPR = D / 4, GR = 64 * W / LPR, ROWS = 4 / W;
   __shared__ __attribute__((aligned(16))) float part[ROWS][GR][D + 4];
   const int kvh = blockIdx.x % v.n_kv;
-  const PagedMerge& mg = merges[blockIdx.x / v.n_kv];
+  const PagedMerge mg = uniform_load(merges + blockIdx.x / v.n_kv);
   const PagedSeq s = mg.s;
   const int which = threadIdx.x / (64 * W), r = blockIdx.y * ROWS + which;
   const int grp = threadIdx.x % (64 * W) / LPR, i = threadIdx.x % LPR * 4;
@@ -596,7 +636,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedView v, const Pag
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = fmaf(a, x[e], o[e]);
   }
-  const int tk = (mg.row0 + r) / v.group, hd = kvh * v.group + mg.row0 + r - tk * v.group;
+  const int tk = quotient(mg.row0 + r, v.by_group), hd = kvh * v.group + mg.row0 + r - tk * v.group;
   const size_t at = (size_t)(s.first + tk) * v.n_head + hd;
   stv4<DT>(out, at * D + i, o / lt);
   if (lse && i == 0) lse[at] = mt * kLn2 + logf(lt);
@@ -633,7 +673,7 @@ __global__ __launch_bounds__(256) void paged_weights_rows_kernel(PagedView v, co
   __shared__ __attribute__((aligned(1024))) char lds[4][KT * RB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15, kvh = blockIdx.y;
-  const PagedSeq s = v.seqs[blockIdx.z];
+  const PagedSeq s = uniform_load(v.seqs + blockIdx.z);
   if (!few_rows<DT>(s.fresh * v.group)) return;
   const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
   const int end = min(s.len, (int)(blockIdx.x + 1) * kWeighKeys);
@@ -644,7 +684,7 @@ __global__ __launch_bounds__(256) void paged_weights_rows_kernel(PagedView v, co
   auto k_swizzle = [](int key) { return LPR == 8 ? (key >> 1) & 7 : key & 15; };
   u32x4_t kr[NV];
   const int lr = lane / LPR, seg = lane % LPR;
-  auto load = [&](int k) {
+  auto load = [&](int k) INLINED {
     uint32_t row[KG];
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) row[kg] = cache_row(v, s, kvh, min(k + kg * 16, last16));
@@ -658,14 +698,14 @@ __global__ __launch_bounds__(256) void paged_weights_rows_kernel(PagedView v, co
   u32x4_t qf[KS];
   float base[4];                                               // of rows r0 + 4g + r: lse in base 2, and the position
   int at[4];
-  auto queries = [&](int r0, int r1) {
-    const int row = min(r0 + n, r1 - 1), token = row / v.group, head = kvh * v.group + row - token * v.group;
+  auto queries = [&](int r0, int r1) INLINED {
+    const int row = min(r0 + n, r1 - 1), token = quotient(row, v.by_group), head = kvh * v.group + row - token * v.group;
     const char* qr = q + (s.first + token) * qs + (size_t)head * RB + g * 16;
 #pragma unroll
     for (int i = 0; i < KS; ++i) qf[i] = *(const u32x4_t*)(qr + i * 64);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int rr = min(r0 + 4 * g + r, r1 - 1), tk = rr / v.group;
+      const int rr = min(r0 + 4 * g + r, r1 - 1), tk = quotient(rr, v.by_group);
       base[r] = lse[(size_t)(s.first + tk) * v.n_head + kvh * v.group + rr - tk * v.group] * kLog2e;
       at[r] = r0 + 4 * g + r < r1 ? before + tk : -1;          // -1: no such row
     }
@@ -707,8 +747,8 @@ __global__ __launch_bounds__(256) void paged_weights_rows_kernel(PagedView v, co
         const int key = k0 + kg * 16 + n;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool seen = key <= at[r] && (v.window <= 0 || key > at[r] - v.window || key < v.sinks);
-          sum[kg] += seen ? __builtin_amdgcn_exp2f(fmaf(sacc[r], c, -base[r])) : 0.f;
+          const bool seen = (key <= at[r]) & ((v.window <= 0) | (key > at[r] - v.window) | (key < v.sinks));
+          sum[kg] += __builtin_amdgcn_exp2f(seen ? fmaf(sacc[r], c, -base[r]) : -INFINITY);
         }
       }
     }
@@ -722,117 +762,116 @@ __global__ __launch_bounds__(256) void paged_weights_rows_kernel(PagedView v, co
   }
 }
 
-// Many rows of queries, 16-bit types; grid = (blocks of 4 * 32 * KW positions, n_kv, n_seq).  A wave holds the K rows of 32 * KW positions as
-// operands and goes through the rows that see any of the block's, 32 at a time, which come to LDS by asynchronous copies, four steps in a ring, for all
-// waves.  S[row][key] as above: a lane adds up 16 rows of its key.  An exponential takes 16 cycles of a wave's vector unit and a product of its
-// 32 x 32 x 16 scores 32 of the matrix unit, eight for d = 128: the products bound it.
-constexpr int kWeighRing = 4;
-template <int DT, int D, int KW>
+// Many rows of queries, 16-bit types; grid = (blocks of 128 positions, n_kv, n_seq).  A wave holds the K rows of 32 positions as operands and goes
+// through the rows that see any of the block's, 64 at a time (two products side by side), which come to LDS by asynchronous copies, three steps in a
+// ring, for all waves.  S[row][key] as above: a lane adds up 16 rows of its key.
+constexpr int kWeighRing = 3, kWeighRows = 64, kWeighTileKeys = 128;
+template <int DT, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_weights_tile_kernel(
     PagedView v, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc, const float* __restrict__ lse, float decay,
     float* __restrict__ w, int64_t ws) {
-  constexpr int RB = D * 2, KS = D / 16, SEG = D / 8, RPC = 64 / SEG, NC = 8 / RPC;      // copies of a wave's 8 rows of a step
-  __shared__ __attribute__((aligned(1024))) char rows_lds[kWeighRing][32 * RB];
-  __shared__ __attribute__((aligned(1024))) float lse_lds[kWeighRing][4][64];
+  constexpr int RB = D * 2, KS = D / 16, SEG = D / 8, RPC = 64 / SEG, NC = kWeighRows / 4 / RPC;      // copies of a wave's rows of a step
+  __shared__ __attribute__((aligned(1024))) char rows_lds[kWeighRing][kWeighRows * RB];
+  __shared__ __attribute__((aligned(1024))) float lse_lds[kWeighRing][4][kWeighRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, n = lane & 31, kvh = blockIdx.y;
-  const PagedSeq s = v.seqs[blockIdx.z];
+  const PagedSeq s = uniform_load(v.seqs + blockIdx.z);
   if (few_rows<DT>(s.fresh * v.group)) return;
-  constexpr int KEYS = 32 * KW;
-  const int kb0 = blockIdx.x * 4 * KEYS;
+  const int kb0 = blockIdx.x * kWeighTileKeys;
   if (kb0 >= s.len) return;
   const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
-  const int k0 = kb0 + wave * KEYS;
-  // rows that see some key of the block, of the wave
-  const int kb1 = min(kb0 + 4 * KEYS, s.len), k1 = min(k0 + KEYS, s.len);
+  const int k0 = kb0 + wave * 32;
+  // rows that see some key of the block: [b0, b1); new tokens that see some key of the wave: [t0, t1)
+  const int kb1 = min(kb0 + kWeighTileKeys, s.len), k1 = min(k0 + 32, s.len);
   const int b0 = first_token(s, kb0) * v.group, b1 = end_token(v, s, kb0, kb1) * v.group;
   const int t0 = first_token(s, k0), t1 = k0 < s.len ? end_token(v, s, k0, k1) : 0;
   const float c = v.scale * kLog2e;
 
-  u32x4_t kf[KW][KS];
-#pragma unroll
-  for (int x = 0; x < KW; ++x) {
-    const int p = min(k0 + x * 32 + (n & 16), last16);
-    const int pl = __builtin_amdgcn_readlane(p, 0), ph = __builtin_amdgcn_readlane(p, 16);
+  u32x4_t kf[KS];
+  {
+    const int pl = min(k0, last16), ph = min(k0 + 16, last16), p = n & 16 ? ph : pl;
     const uint32_t rl = cache_row(v, s, kvh, pl), rh = cache_row(v, s, kvh, ph);
     const char* kr = kc + (size_t)((n & 16 ? rh : rl) + min(n & 15, s.len - 1 - p)) * RB + h * 16;
 #pragma unroll
-    for (int i = 0; i < KS; ++i) kf[x][i] = *(const u32x4_t*)(kr + i * 32);
+    for (int i = 0; i < KS; ++i) kf[i] = *(const u32x4_t*)(kr + i * 32);
   }
   auto swizzle = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
-  auto issue = [&](int u) {
-    const int r0 = b0 + u * 32, ta = r0 / v.group;              // the step's first token: offsets from there fit 32 bits
+  auto issue = [&](int u) INLINED {
+    const int r0 = b0 + u * kWeighRows, ta = quotient(r0, v.by_group);              // the step's first token: offsets from there fit 32 bits
     const char* qb = q + (s.first + ta) * qs + (size_t)kvh * v.group * RB;
+    auto from = [&](int r, int per_token, int per_head) INLINED {
+      const int row = min(r0 + r, b1 - 1), token = quotient(row, v.by_group);
+      return (uint32_t)((token - ta) * per_token + (row - token * v.group) * per_head);
+    };
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      const int r = wave * 8 + j * RPC + lane / SEG, row = min(r0 + r, b1 - 1), token = row / v.group;
-      copy_to_lds(qb, (uint32_t)((token - ta) * (int)qs + (row - token * v.group) * RB) + ((lane % SEG) ^ swizzle(r)) * 16,
-                  (u32x4_t*)(rows_lds[u % kWeighRing] + (wave * 8 + j * RPC) * RB));
+      const int r = (wave * NC + j) * RPC + lane / SEG;
+      copy_to_lds(qb, from(r, (int)qs, RB) + ((lane % SEG) ^ swizzle(r)) * 16, (u32x4_t*)(rows_lds[u % kWeighRing] + (wave * NC + j) * 1024));
     }
-    const int row = min(r0 + n, b1 - 1), token = row / v.group;
-    copy_words_to_lds((const char*)(lse + (size_t)(s.first + ta) * v.n_head + kvh * v.group),
-                      (uint32_t)(((token - ta) * v.n_head + row - token * v.group) * 4), lse_lds[u % kWeighRing][wave]);
+    copy_words_to_lds((const char*)(lse + (size_t)(s.first + ta) * v.n_head + kvh * v.group), from(lane, v.n_head * 4, 4),
+                      lse_lds[u % kWeighRing][wave]);
   };
-  const int steps = b1 > b0 ? (b1 - b0 + 31) / 32 : 0;
-  float sum[KW];
-#pragma unroll
-  for (int x = 0; x < KW; ++x) sum[x] = 0.f;
+  const uint32_t qaddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&rows_lds[0][0] + (uint32_t)(n * RB + (h ^ swizzle(n)) * 16);
+  const uint32_t laddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)&lse_lds[0][wave][0] + h * 16;
+  const int steps = b1 > b0 ? (b1 - b0 + kWeighRows - 1) / kWeighRows : 0;
+  float sum[2] = {0.f, 0.f};
 #pragma unroll
   for (int u = 0; u < kWeighRing - 1; ++u)
     if (u < steps) issue(u);
   for (int u = 0; u < steps; ++u) {
     copies_barrier<(NC + 1) * (kWeighRing - 2)>(u + kWeighRing - 2 >= steps);
     if (u + kWeighRing - 1 < steps) issue(u + kWeighRing - 1);
-    const int r0 = b0 + u * 32, ta = r0 / v.group, tb = min(r0 + 31, b1 - 1) / v.group;
+    const int r0 = b0 + u * kWeighRows, ta = quotient(r0, v.by_group), tb = quotient(min(r0 + kWeighRows - 1, b1 - 1), v.by_group);
     if (tb < t0 || ta >= t1) continue;
-    const char* ql = rows_lds[u % kWeighRing] + n * RB;
-    const float* ll = lse_lds[u % kWeighRing][wave];
-    f32x16_t sacc[KW];
+    f32x16_t sacc[2];
 #pragma unroll
-    for (int x = 0; x < KW; ++x)
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sacc[x][i] = 0.f;
+    uint32_t qa[KS];
+    u32x4_t qf[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const u32x4_t qf = *(const u32x4_t*)(ql + ((ks * 2 + h) ^ swizzle(n)) * 16);
+    for (int ks = 0; ks < KS; ++ks) qa[ks] = (qaddr + (u % kWeighRing) * (uint32_t)sizeof(rows_lds[0])) ^ (ks * 32);
+    read_pieces<0>(qa, qf);
 #pragma unroll
-      for (int x = 0; x < KW; ++x) sacc[x] = mfma32<DT>(qf, kf[x][ks], sacc[x]);
-    }
-    float base[16];
+    for (int ks = 0; ks < KS; ++ks) sacc[0] = mfma32<DT>(qf[ks], kf[ks], sacc[0]);
+    read_pieces<32 * RB>(qa, qf);
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const f32x4_t b = ld4(ll + 2 * i + 4 * h);
+    for (int ks = 0; ks < KS; ++ks) sacc[1] = mfma32<DT>(qf[ks], kf[ks], sacc[1]);
+    u32x4_t bits[2][4];                       // lse of the lane's rows 8 i + 4 h + .. of either product
+    uint32_t la[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) base[i + e] = b[e] * kLog2e;
-    }
-    const bool full = k0 + KEYS - 1 <= before + ta && r0 + 32 <= b1 &&
-                      (v.window <= 0 || k0 > before + tb - v.window || k0 + KEYS <= v.sinks);
-    if (full) {
+    for (int i = 0; i < 4; ++i) la[i] = laddr + (u % kWeighRing) * (uint32_t)sizeof(lse_lds[0]) + i * 32;
+    read_pieces<0>(la, bits[0]);
+    read_pieces<128>(la, bits[1]);
+    const bool full = k0 + 31 <= before + ta && r0 + kWeighRows <= b1 && (v.window <= 0 || k0 > before + tb - v.window || k0 + 32 <= v.sinks);
+    auto add = [&](auto whole) INLINED {
+      constexpr bool WHOLE = decltype(whole)::value;
+      const int key = k0 + n;
 #pragma unroll
-      for (int x = 0; x < KW; ++x)
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum[x] += __builtin_amdgcn_exp2f(fmaf(sacc[x][i], c, -base[i]));
-    } else {
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4_t base = __builtin_bit_cast(f32x4_t, bits[x][i / 4]) * kLog2e;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = r0 + (i & 3) + 8 * (i >> 2) + 4 * h, pos = row < b1 ? before + row / v.group : -1;
-#pragma unroll
-        for (int x = 0; x < KW; ++x) {
-          const int key = k0 + x * 32 + n;
-          const bool seen = key <= pos && (v.window <= 0 || key > pos - v.window || key < v.sinks);
-          sum[x] += seen ? __builtin_amdgcn_exp2f(fmaf(sacc[x][i], c, -base[i])) : 0.f;
+          for (int e = 0; e < 4; ++e) {
+            float p = fmaf(sacc[x][i + e], c, -base[e]);
+            if constexpr (!WHOLE) {
+              const int row = r0 + x * 32 + 2 * i + 4 * h + e, pos = row < b1 ? before + quotient(row, v.by_group) : -1;
+              p = ((key <= pos) & ((v.window <= 0) | (key > pos - v.window) | (key < v.sinks))) ? p : -INFINITY;
+            }
+            sum[x] += __builtin_amdgcn_exp2f(p);
+          }
         }
-      }
-    }
+    };
+    if (full) add(std::true_type{});
+    else add(std::false_type{});
   }
-#pragma unroll
-  for (int x = 0; x < KW; ++x) {
-    const float t = sum_partner<32>(sum[x]);
-    const int key = k0 + x * 32 + n;
-    if (h == 0 && key < s.len) {
-      float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + key;
-      *to = new_weight(t, decay != 0.f && key < before ? *to : 0.f, decay, key >= before);
-    }
+  const float t = sum_partner<32>(sum[0] + sum[1]);
+  const int key = k0 + n;
+  if (h == 0 && key < s.len) {
+    float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + key;
+    *to = new_weight(t, decay != 0.f && key < before ? *to : 0.f, decay, key >= before);
   }
 }
 
@@ -1011,7 +1050,7 @@ hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t q
     if (few) paged_weights_rows_kernel<DT, D><<<dim3((v.longest + kWeighKeys - 1) / kWeighKeys, v.n_kv, v.n_seq), 256, 0, st>>>(
         v, (const char*)q, qb, (const char*)kc, lse, decay, w, ws);
     if constexpr (DT != DT_F32)
-      if (many) paged_weights_tile_kernel<DT, D, 1><<<dim3((v.longest + 127) / 128, v.n_kv, v.n_seq), 256, 0, st>>>(
+      if (many) paged_weights_tile_kernel<DT, D><<<dim3((v.longest + kWeighTileKeys - 1) / kWeighTileKeys, v.n_kv, v.n_seq), 256, 0, st>>>(
           v, (const char*)q, qb, (const char*)kc, lse, decay, w, ws);
   });
   return hipGetLastError();

@@ -9,6 +9,19 @@ constexpr int kRowTile = 16;        // query rows (token x head of a group) of a
 inline int row_keys(int dtype) { return dtype == 0 ? 16 : 32; }    // keys of a step of it: 32 of 16-bit caches, 16 of fp32 ones
 constexpr int kTileRows = 128, kTileKeys = 64;                     // the same of the tile kernel (16-bit types)
 
+// Quotients by a number known on the host: x / d = floor(x m / 2^(31 + l)) for 0 <= x < 2^31, with l = ceil(log2 d), m = ceil(2^(31 + l) / d), since
+// m d exceeds 2^(31 + l) by less than d <= 2^l (division by invariant multiplication; Granlund and Montgomery, PLDI 1994).
+struct Divisor {
+  uint32_t m;
+  int l;
+};
+inline Divisor divisor(int d) {
+  int l = 0;
+  while ((1ll << l) < d) ++l;
+  return {(uint32_t)(((1ull << (31 + l)) + d - 1) / d), l};
+}
+__device__ __forceinline__ int quotient(int x, const Divisor& d) { return (int)(__umulhi((uint32_t)x << 1, d.m) >> d.l); }
+
 // A sequence of the plan.
 struct PagedSeq {
   int first;      // its first new token's row in q, k, v and out
@@ -40,7 +53,8 @@ struct PagedView {     // device memory of a plan, and the shape
   const uint32_t* places;      // [T] row of a new token in the cache, key head 0
   float *pm, *po;              // partial results: (max, sum) of a row, its [head_dim]
   int n_seq, tokens, longest;
-  int n_head, n_kv, group, d, page_size, page_shift;   // page_shift -1: page_size is not a power of two
+  int n_head, n_kv, group, d, page_size;
+  Divisor by_group, by_page;
   int window, sinks;
   float scale;
 };

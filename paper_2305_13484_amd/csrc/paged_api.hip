@@ -252,7 +252,8 @@ struct flover_paged_plan {
     v.group = shape.n_head / shape.n_kv_head;
     v.d = shape.head_dim;
     v.page_size = shape.page_size;
-    v.page_shift = (shape.page_size & (shape.page_size - 1)) == 0 ? __builtin_ctz(shape.page_size) : -1;
+    v.by_group = flk::divisor(v.group);
+    v.by_page = flk::divisor(v.page_size);
     v.window = shape.window;
     v.sinks = shape.window > 0 ? shape.sinks : 0;
     v.scale = 1.0f / std::sqrt((float)shape.head_dim);
