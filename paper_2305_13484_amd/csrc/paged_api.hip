@@ -63,7 +63,8 @@ struct Lists {
   size_t pm = 0, po = 0, total = 0;                        // partial results, behind the lists
   int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_tiles = 0, n_merges = 0;
   int most_parts = 0, most_rows = 0;                       // of a merge
-  bool few = false, many = false;                          // sequences of up to 16 rows per key head (of fp32: all), of more
+  bool few = false, many = false;                          // sequences of up to 16 rows per key head (of fp32: all), of more,
+  int64_t row_blocks = 0, tile_blocks = 0;                 // and their blocks of 512, of 128 positions of a key head
   bool shared = false, shared_new = false;                 // a page twice in use; one that new tokens go to
 };
 
@@ -105,7 +106,13 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   for (int i = 0; i < n_seq; ++i) {
     const int need = (len[i] + sh.page_size - 1) / sh.page_size, fresh = len[i] - new_len[i];
     seqs[i] = {first, new_len[i], len[i], (int)pages.size()};
-    (sh.dtype == FLOVER_F32 || new_len[i] * group <= flk::kRowTile ? L->few : L->many) = true;
+    if (sh.dtype == FLOVER_F32 || (int64_t)new_len[i] * group <= flk::kRowTile) {
+      L->few = true;
+      L->row_blocks += ((int64_t)len[i] + 511) / 512 * sh.n_kv_head;
+    } else {
+      L->many = true;
+      L->tile_blocks += ((int64_t)len[i] + 127) / 128 * sh.n_kv_head;
+    }
     for (int p = 0; p < need; ++p) {
       const int page = table[(size_t)i * stride + p];
       const bool written = new_len[i] > 0 && (int64_t)(p + 1) * sh.page_size > fresh;
@@ -455,7 +462,7 @@ int32_t flover_k_paged_weights(const flover_paged_plan* plan, const void* q, int
       return fail_call(FLOVER_E_INVAL, "the weights share memory with what is read");
     PAGED_TRY(ready(plan, (hipStream_t)stream));
     PAGED_HIP(flk::paged_weights(plan->shape.dtype, plan->view(), q, q_stride, kcache, lse, decay, weights, weight_stride, l.few,
-                                 l.many, (hipStream_t)stream));
+                                 l.row_blocks < 1024, l.many, l.tile_blocks <= 128, (hipStream_t)stream));
     return FLOVER_OK;
   });
 }
