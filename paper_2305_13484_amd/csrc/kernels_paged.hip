@@ -921,15 +921,18 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 // A block per (key head, sequence).  The weight of the last row kept is found digit by digit from the top (four digits of 8 bits, counted
-// in LDS); rows of exactly that weight are taken from the front.  Then the positions are gone through in order, 1024 at a time, and numbered.
+// in LDS); rows of exactly that weight are taken from the front.  Then the positions are gone through in order, 1024 at a time, and numbered.  The
+// weights' keys stay in LDS (the first kKeysHeld of them; of a longer sequence the rest is read again).
+constexpr int kKeysHeld = 12288;
 __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const float* w, int64_t ws, int budget, int first,
                                                             int recent, float* wo, int64_t os, int* __restrict__ kept) {
+  __shared__ uint32_t held[kKeysHeld];
   __shared__ int count[256];
   __shared__ int found[2];                 // digit, rows still wanted of it
-  __shared__ int waves[16][2];
+  __shared__ int waves[2][16][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const size_t at = (size_t)blockIdx.y * v.n_kv + blockIdx.x;
-  const int len = v.seqs[blockIdx.y].len;
+  const int len = uniform_load(&v.seqs[blockIdx.y].len);
   const float* mine = w + at * ws;
   float* to = wo ? wo + at * os : nullptr;
   int* keep = kept + at * budget;
@@ -940,20 +943,32 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const f
     }
     return;
   }
+  if (tid < 256) count[tid] = 0;
+  for (int p0 = 0; p0 < min(len, kKeysHeld); p0 += 4096) {      // four loads on their way at a time
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = mine[min(p0 + j * 1024 + tid, len - 1)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (p0 + j * 1024 + tid < min(len, kKeysHeld)) held[p0 + j * 1024 + tid] = weight_key(x[j]);
+  }
+  auto key_of = [&](int p) INLINED { return p < kKeysHeld ? held[p] : weight_key(mine[p]); };
   const int sure = first + recent;         // of the others, `wanted` are kept
   int wanted = budget - sure;
   uint32_t prefix = 0;
   for (int shift = 24; shift >= 0 && wanted > 0; shift -= 8) {
-    if (tid < 256) count[tid] = 0;
     __syncthreads();
     for (int p = first + tid; p < len - recent; p += 1024) {
-      const uint32_t k = weight_key(mine[p]);
+      const uint32_t k = key_of(p);
       if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&count[k >> shift & 255], 1);
     }
     __syncthreads();
     if (wave == 0) {                       // lane l: digits 255 - 4l and the three below
       int c[4], sum = 0;
-      for (int i = 0; i < 4; ++i) sum += c[i] = count[255 - 4 * lane - i];
+      for (int i = 0; i < 4; ++i) {
+        sum += c[i] = count[255 - 4 * lane - i];
+        count[255 - 4 * lane - i] = 0;
+      }
       int upto = sum;
       for (int dlt = 1; dlt < 64; dlt <<= 1) {
         const int o = __shfl_up(upto, dlt, 64);
@@ -969,73 +984,89 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const f
     __syncthreads();
     prefix |= (uint32_t)found[0] << shift;
     wanted = found[1];
-    __syncthreads();
   }
   // heavier than prefix: kept; equal: the first `wanted`
   int ranks = 0, ties = 0;                 // kept, and equal ones met, so far
-  for (int p0 = 0; p0 < len; p0 += 1024) {
+  for (int p0 = 0, turn = 0; p0 < len; p0 += 1024, turn ^= 1) {
     const int p = p0 + tid;
-    const float x = p < len ? mine[p] : 0.f;
+    const float x = to && p < len ? mine[p] : 0.f;
     const bool certain = p < len && (p < first || p >= len - recent);
     const bool middle = p < len && !certain && budget > sure;
-    const uint32_t k = weight_key(x);
-    const bool tie = middle && k == prefix;
-    const uint64_t tb = __ballot(tie);
-    const uint64_t below = (1ull << lane) - 1;
-    if (lane == 0) waves[wave][0] = __popcll(tb);
-    __syncthreads();
-    int t = ties;
-    for (int i = 0; i < 16; ++i) {
-      if (i < wave) t += waves[i][0];
-      ties += waves[i][0];
+    const uint32_t k = p < len ? key_of(p) : 0u;
+    const bool tie = middle && k == prefix, above = certain || (middle && k > prefix);
+    const uint64_t below = (1ull << lane) - 1, tb = __ballot(tie), ab = __ballot(above);
+    if (lane == 0) {
+      waves[turn][wave][0] = __popcll(tb);
+      waves[turn][wave][1] = __popcll(ab);
     }
-    const bool take = certain || (middle && k > prefix) || (tie && t + __popcll(tb & below) < wanted);
-    const uint64_t kb = __ballot(take);
-    if (lane == 0) waves[wave][1] = __popcll(kb);
-    __syncthreads();
-    int r = ranks;
+    __syncthreads();                       // (the other turn's counts are read before the next barrier)
+    // in front of the wave: equal ones, of which the first `wanted` are kept, and heavier ones
+    int t = ties, r = ranks;
     for (int i = 0; i < 16; ++i) {
-      if (i < wave) r += waves[i][1];
-      ranks += waves[i][1];
+      const int e = waves[turn][i][0], more = waves[turn][i][1] + max(0, min(e, wanted - ties));
+      if (i < wave) {
+        t += e;
+        r += more;
+      }
+      ties += e;
+      ranks += more;
     }
-    r += __popcll(kb & below);
-    if (take) {
+    const int mine_t = t + __popcll(tb & below);                 // equal ones in front of the lane
+    if (above || (tie && mine_t < wanted)) {
+      r += __popcll(ab & below) + max(0, min(mine_t, wanted) - min(t, wanted));
       keep[r] = p;
-      if (to) to[r] = x;                   // at or in front of p: behind the barriers nobody reads that place any more
+      if (to) to[r] = x;                   // at or in front of p: behind the barrier nobody reads that place any more
     }
   }
 }
 
 // The kept rows to the front: block = (128 bytes of a row, key head, sequence x K|V), 256 threads, 8 per row, kMove rows of each thread at a time.
 // A row moves to a place at or in front of its own, and a place is overwritten only once every row up to it has been read: a
-// barrier between the reads (waited for) and the writes of a batch is enough, because the batch behind reads from places behind.
+// barrier between the reads (waited for) and the writes of a batch is enough, because the batch behind reads from places behind.  Where the rows of
+// the next batch lie and go is looked up, a row per thread, while a batch is read.
 constexpr int kMove = 8;
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedView v, char* kc, char* vc, int budget, int first,
                                                          const int* __restrict__ kept, int row_bytes) {
-  const PagedSeq s = v.seqs[blockIdx.z >> 1];
+  constexpr int STEP = 32 * kMove;
+  __shared__ uint2 rows[2][STEP];            // of a batch, in turns: (from, to)
+  const PagedSeq s = uniform_load(v.seqs + (blockIdx.z >> 1));
   if (s.len <= budget) return;
-  const int kvh = blockIdx.y;
-  char* cache = (blockIdx.z & 1 ? vc : kc) + blockIdx.x * 128 + (threadIdx.x & 7) * 16;
+  const int kvh = blockIdx.y, tid = threadIdx.x;
+  char* cache = (blockIdx.z & 1 ? vc : kc) + blockIdx.x * 128 + (tid & 7) * 16;
   const int* keep = kept + ((size_t)(blockIdx.z >> 1) * v.n_kv + kvh) * budget;
-  for (int r0 = first; r0 < budget; r0 += 32 * kMove) {
+  auto position = [&](int r0) INLINED { return keep[min(r0 + tid, budget - 1)]; };
+  struct Page {
+    int from, to;
+  };
+  auto pages = [&](int pos, int r0) INLINED {
+    return Page{v.pages[s.pages + quotient(pos, v.by_page)], v.pages[s.pages + quotient(min(r0 + tid, budget - 1), v.by_page)]};
+  };
+  auto row = [&](int page, int pos) INLINED { return ((uint32_t)page * v.n_kv + kvh) * v.page_size + (pos - quotient(pos, v.by_page) * v.page_size); };
+  auto put = [&](int turn, const Page& pg, int pos, int r0) INLINED {
+    rows[turn][tid] = make_uint2(row(pg.from, pos), row(pg.to, min(r0 + tid, budget - 1)));
+  };
+  int pos = position(first);
+  put(0, pages(pos, first), pos, first);
+  pos = position(first + STEP);
+  __syncthreads();
+  for (int r0 = first, turn = 0; r0 < budget; r0 += STEP, turn ^= 1) {
+    const Page ahead = pages(pos, r0 + STEP);
     u32x4_t x[kMove];
-    int src[kMove];
+    uint32_t to[kMove];
 #pragma unroll
     for (int j = 0; j < kMove; ++j) {
-      const int r = r0 + j * 32 + (threadIdx.x >> 3);
-      src[j] = r < budget ? keep[r] : r;
+      const uint2 ft = rows[turn][j * 32 + (tid >> 3)];
+      to[j] = ft.y;
+      x[j] = *(const u32x4_t*)(cache + (size_t)ft.x * row_bytes);
     }
+    put(turn ^ 1, ahead, pos, r0 + STEP);
+    pos = position(r0 + 2 * STEP);
 #pragma unroll
-    for (int j = 0; j < kMove; ++j) {
-      const int r = r0 + j * 32 + (threadIdx.x >> 3);
-      if (src[j] != r) x[j] = *(const u32x4_t*)(cache + (size_t)cache_row(v, s, kvh, src[j]) * row_bytes);
-    }
-    copies_barrier<0>(true);
+    for (int j = 0; j < kMove; ++j) asm volatile("" : "+v"(x[j]));      // has been read
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kMove; ++j) {
-      const int r = r0 + j * 32 + (threadIdx.x >> 3);
-      if (src[j] != r) *(u32x4_t*)(cache + (size_t)cache_row(v, s, kvh, r) * row_bytes) = x[j];
-    }
+    for (int j = 0; j < kMove; ++j)
+      if (r0 + j * 32 + (tid >> 3) < budget) *(u32x4_t*)(cache + (size_t)to[j] * row_bytes) = x[j];
   }
 }
 
