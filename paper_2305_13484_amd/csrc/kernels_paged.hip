@@ -921,16 +921,24 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 // A block per (key head, sequence).  The weight of the last row kept is found digit by digit from the top (four digits of 8 bits, counted
-// in LDS); rows of exactly that weight are taken from the front.  Then the positions are gone through in order, 1024 at a time, and numbered.  The
+// in LDS); rows of exactly that weight are taken from the front.  Then the positions are gone through in order, four per thread, and numbered.  The
 // weights' keys stay in LDS (the first kKeysHeld of them; of a longer sequence the rest is read again).
-constexpr int kKeysHeld = 12288;
+constexpr int kKeysHeld = 18432;           // 72 KB: two blocks per compute unit
+// Sums over the lanes up to and including one's own, of the wave; lanes without a source add zero.
+template <int CTRL, int ROWS> __device__ __forceinline__ int plus_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int scan16(int x) {               // within 16 lanes: row_shr 1, 2, 4, 8
+  return plus_dpp<0x118, 0xf>(plus_dpp<0x114, 0xf>(plus_dpp<0x112, 0xf>(plus_dpp<0x111, 0xf>(x))));
+}
+__device__ __forceinline__ int scan64(int x) {               // lane 15 of rows 0 and 2 to rows 1 and 3, lane 31 to rows 2 and 3
+  return plus_dpp<0x143, 0xc>(plus_dpp<0x142, 0xa>(scan16(x)));
+}
 __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const float* w, int64_t ws, int budget, int first,
                                                             int recent, float* wo, int64_t os, int* __restrict__ kept) {
   __shared__ uint32_t held[kKeysHeld];
   __shared__ int count[256];
-  __shared__ int found[2];                 // digit, rows still wanted of it
+  __shared__ int found[3];                 // digit, rows still wanted of it, whether those are all
   __shared__ int waves[2][16][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t at = (size_t)blockIdx.y * v.n_kv + blockIdx.x;
   const int len = uniform_load(&v.seqs[blockIdx.y].len);
   const float* mine = w + at * ws;
@@ -956,7 +964,8 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const f
   const int sure = first + recent;         // of the others, `wanted` are kept
   int wanted = budget - sure;
   uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0 && wanted > 0; shift -= 8) {
+  bool whole = false;
+  for (int shift = 24; shift >= 0 && wanted > 0 && !whole; shift -= 8) {
     __syncthreads();
     for (int p = first + tid; p < len - recent; p += 1024) {
       const uint32_t k = key_of(p);
@@ -969,104 +978,123 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const f
         sum += c[i] = count[255 - 4 * lane - i];
         count[255 - 4 * lane - i] = 0;
       }
-      int upto = sum;
-      for (int dlt = 1; dlt < 64; dlt <<= 1) {
-        const int o = __shfl_up(upto, dlt, 64);
-        if (lane >= dlt) upto += o;
-      }
+      const int upto = scan64(sum);
       if (lane == __builtin_ctzll(__ballot(upto >= wanted))) {      // the rows under way are more than `wanted`
         int left = wanted - (upto - sum), i = 0;
         while (i < 3 && c[i] < left) left -= c[i++];
         found[0] = 255 - 4 * lane - i;
         found[1] = left;
+        found[2] = left == c[i];            // every row that begins with these digits: the others need not be known
       }
     }
     __syncthreads();
     prefix |= (uint32_t)found[0] << shift;
     wanted = found[1];
+    whole = found[2];
   }
-  // heavier than prefix: kept; equal: the first `wanted`
+  // heavier than prefix (or as heavy, where all of those are kept): kept; equal: the first `wanted`
   int ranks = 0, ties = 0;                 // kept, and equal ones met, so far
-  for (int p0 = 0, turn = 0; p0 < len; p0 += 1024, turn ^= 1) {
-    const int p = p0 + tid;
-    const float x = to && p < len ? mine[p] : 0.f;
-    const bool certain = p < len && (p < first || p >= len - recent);
-    const bool middle = p < len && !certain && budget > sure;
-    const uint32_t k = p < len ? key_of(p) : 0u;
-    const bool tie = middle && k == prefix, above = certain || (middle && k > prefix);
-    const uint64_t below = (1ull << lane) - 1, tb = __ballot(tie), ab = __ballot(above);
-    if (lane == 0) {
-      waves[turn][wave][0] = __popcll(tb);
-      waves[turn][wave][1] = __popcll(ab);
+  for (int p0 = 0, turn = 0; p0 < len; p0 += 4096, turn ^= 1) {
+    const int first_p = p0 + tid * 4;
+    float x[4];
+    uint32_t above = 0, tie = 0;           // bits: of the thread's four positions
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int p = first_p + j;
+      x[j] = to && p < len ? mine[p] : 0.f;
+      const uint32_t k = p < len ? key_of(p) : 0u;
+      const bool certain = p < len && (p < first || p >= len - recent), middle = p < len && !certain && budget > sure;
+      above |= (uint32_t)(certain || (middle && (k > prefix || (whole && k == prefix)))) << j;
+      tie |= (uint32_t)(middle && !whole && k == prefix) << j;
+    }
+    const int te = __popc(tie), ta = __popc(above), se = scan64(te), sa = scan64(ta);
+    if (lane == 63) {
+      waves[turn][wave][0] = se;
+      waves[turn][wave][1] = sa;
     }
     __syncthreads();                       // (the other turn's counts are read before the next barrier)
-    // in front of the wave: equal ones, of which the first `wanted` are kept, and heavier ones
-    int t = ties, r = ranks;
-    for (int i = 0; i < 16; ++i) {
-      const int e = waves[turn][i][0], more = waves[turn][i][1] + max(0, min(e, wanted - ties));
-      if (i < wave) {
-        t += e;
-        r += more;
+    // in front of the wave: equal ones, of which the first `wanted` are kept, and kept ones.  Lane i sums up for wave i
+    const int e = lane < 16 ? waves[turn][lane][0] : 0, e_upto = scan16(e);
+    const int more = lane < 16 ? waves[turn][lane][1] + max(0, min(e, wanted - ties - (e_upto - e))) : 0, more_upto = scan16(more);
+    const int of_wave = ties + __builtin_amdgcn_readlane(e_upto - e, wave);
+    int t = of_wave + se - te;
+    int r = ranks + __builtin_amdgcn_readlane(more_upto - more, wave) + (sa - ta) + min(t, wanted) - min(of_wave, wanted);
+    ties += __builtin_amdgcn_readlane(e_upto, 15);
+    ranks += __builtin_amdgcn_readlane(more_upto, 15);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool equal = tie >> j & 1;
+      if ((above >> j & 1) || (equal && t < wanted)) {
+        keep[r] = first_p + j;
+        if (to) to[r] = x[j];              // at or in front of its own: behind the barrier nobody reads that place any more
+        ++r;
       }
-      ties += e;
-      ranks += more;
-    }
-    const int mine_t = t + __popcll(tb & below);                 // equal ones in front of the lane
-    if (above || (tie && mine_t < wanted)) {
-      r += __popcll(ab & below) + max(0, min(mine_t, wanted) - min(t, wanted));
-      keep[r] = p;
-      if (to) to[r] = x;                   // at or in front of p: behind the barrier nobody reads that place any more
+      t += equal;
     }
   }
 }
 
-// The kept rows to the front: block = (128 bytes of a row, key head, sequence x K|V), 256 threads, 8 per row, kMove rows of each thread at a time.
+// The kept rows to the front: block = (PIECES x 16 bytes of a row, key head, sequence x K|V), 256 threads, PIECES per row, kMove rows of each thread
+// at a time.
 // A row moves to a place at or in front of its own, and a place is overwritten only once every row up to it has been read: a
 // barrier between the reads (waited for) and the writes of a batch is enough, because the batch behind reads from places behind.  Where the rows of
 // the next batch lie and go is looked up, a row per thread, while a batch is read.
+// 128 bytes of a row where there are blocks enough, otherwise 32: four times the blocks, and a quarter of the batches one after the other.
 constexpr int kMove = 8;
+template <int PIECES>
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedView v, char* kc, char* vc, int budget, int first,
                                                          const int* __restrict__ kept, int row_bytes) {
-  constexpr int STEP = 32 * kMove;
+  constexpr int PER = 256 / PIECES, STEP = PER * kMove, EACH = STEP / 256;      // rows of a pass, of a batch, of a batch per thread
   __shared__ uint2 rows[2][STEP];            // of a batch, in turns: (from, to)
   const PagedSeq s = uniform_load(v.seqs + (blockIdx.z >> 1));
   if (s.len <= budget) return;
   const int kvh = blockIdx.y, tid = threadIdx.x;
-  char* cache = (blockIdx.z & 1 ? vc : kc) + blockIdx.x * 128 + (tid & 7) * 16;
+  char* cache = (blockIdx.z & 1 ? vc : kc) + blockIdx.x * (PIECES * 16) + tid % PIECES * 16;
   const int* keep = kept + ((size_t)(blockIdx.z >> 1) * v.n_kv + kvh) * budget;
-  auto position = [&](int r0) INLINED { return keep[min(r0 + tid, budget - 1)]; };
-  struct Page {
-    int from, to;
+  struct Lookup {
+    int pos[EACH], from[EACH], to[EACH];
   };
-  auto pages = [&](int pos, int r0) INLINED {
-    return Page{v.pages[s.pages + quotient(pos, v.by_page)], v.pages[s.pages + quotient(min(r0 + tid, budget - 1), v.by_page)]};
+  auto positions = [&](Lookup& a, int r0) INLINED {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) a.pos[i] = keep[min(r0 + i * 256 + tid, budget - 1)];
+  };
+  auto pages = [&](Lookup& a, int r0) INLINED {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      a.from[i] = v.pages[s.pages + quotient(a.pos[i], v.by_page)];
+      a.to[i] = v.pages[s.pages + quotient(min(r0 + i * 256 + tid, budget - 1), v.by_page)];
+    }
   };
   auto row = [&](int page, int pos) INLINED { return ((uint32_t)page * v.n_kv + kvh) * v.page_size + (pos - quotient(pos, v.by_page) * v.page_size); };
-  auto put = [&](int turn, const Page& pg, int pos, int r0) INLINED {
-    rows[turn][tid] = make_uint2(row(pg.from, pos), row(pg.to, min(r0 + tid, budget - 1)));
+  auto put = [&](int turn, const Lookup& a, int r0) INLINED {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      rows[turn][i * 256 + tid] = make_uint2(row(a.from[i], a.pos[i]), row(a.to[i], min(r0 + i * 256 + tid, budget - 1)));
   };
-  int pos = position(first);
-  put(0, pages(pos, first), pos, first);
-  pos = position(first + STEP);
+  Lookup ahead;
+  positions(ahead, first);
+  pages(ahead, first);
+  put(0, ahead, first);
+  positions(ahead, first + STEP);
   __syncthreads();
   for (int r0 = first, turn = 0; r0 < budget; r0 += STEP, turn ^= 1) {
-    const Page ahead = pages(pos, r0 + STEP);
+    pages(ahead, r0 + STEP);
     u32x4_t x[kMove];
     uint32_t to[kMove];
 #pragma unroll
     for (int j = 0; j < kMove; ++j) {
-      const uint2 ft = rows[turn][j * 32 + (tid >> 3)];
+      const uint2 ft = rows[turn][j * PER + tid / PIECES];
       to[j] = ft.y;
       x[j] = *(const u32x4_t*)(cache + (size_t)ft.x * row_bytes);
     }
-    put(turn ^ 1, ahead, pos, r0 + STEP);
-    pos = position(r0 + 2 * STEP);
+    put(turn ^ 1, ahead, r0 + STEP);
+    positions(ahead, r0 + 2 * STEP);
 #pragma unroll
     for (int j = 0; j < kMove; ++j) asm volatile("" : "+v"(x[j]));      // has been read
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kMove; ++j)
-      if (r0 + j * 32 + (tid >> 3) < budget) *(u32x4_t*)(cache + (size_t)to[j] * row_bytes) = x[j];
+      if (r0 + j * PER + tid / PIECES < budget) *(u32x4_t*)(cache + (size_t)to[j] * row_bytes) = x[j];
   }
 }
 
@@ -1138,8 +1166,13 @@ hipError_t paged_evict(int dtype, const PagedView& v, void* kc, void* vc, const 
                        float* wo, int64_t os, int* kept, hipStream_t st) {
   paged_select_kernel<<<dim3(v.n_kv, v.n_seq), 1024, 0, st>>>(v, w, ws, budget, first, recent, wo, os, kept);
   const int row_bytes = v.d * element_bytes(dtype);
-  if (v.longest > budget)
-    paged_move_kernel<<<dim3(row_bytes / 128, v.n_kv, 2 * v.n_seq), 256, 0, st>>>(v, (char*)kc, (char*)vc, budget, first, kept, row_bytes);
+  if (v.longest > budget) {
+    const int heads = 2 * v.n_seq * v.n_kv;
+    if (heads * (row_bytes / 128) >= 256)
+      paged_move_kernel<8><<<dim3(row_bytes / 128, v.n_kv, 2 * v.n_seq), 256, 0, st>>>(v, (char*)kc, (char*)vc, budget, first, kept, row_bytes);
+    else
+      paged_move_kernel<2><<<dim3(row_bytes / 32, v.n_kv, 2 * v.n_seq), 256, 0, st>>>(v, (char*)kc, (char*)vc, budget, first, kept, row_bytes);
+  }
   return hipGetLastError();
 }
 
