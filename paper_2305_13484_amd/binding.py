@@ -502,7 +502,8 @@ class PagedPlan:
         handle = C.c_void_p()
         _check(load_library().flover_k_paged_plan_create(C.byref(self._shape), C.byref(handle)))
         self._handle = handle
-        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = torch.cuda.current_device()
+        self.device = torch.device("cuda", self.index)
         self._cache_shape = (n_pages, n_kv_head, page_size, head_dim)
         self._set(lists)
 
@@ -556,12 +557,13 @@ class PagedPlan:
     def _on(self, *tensors):
         """Stream of a call on these tensors."""
         for t in tensors:
-            if t.device != self.device:
+            if t.get_device() != self.index:                       # -1: on the CPU
                 raise FloverError("tensor on %s, plan on %s" % (t.device, self.device))
-        stream = torch.cuda.current_stream(self.device)
-        if stream.cuda_stream != self.stream:
+        stream = torch.cuda.current_stream(self.index)
+        handle = stream.cuda_stream
+        if handle != self.stream:
             self.memory.record_stream(stream)
-        return stream.cuda_stream
+        return handle
 
     def _cache(self, t: torch.Tensor, name: str) -> int:
         if t.shape != self._cache_shape or t.dtype != self.dtype or not t.is_contiguous():
@@ -591,7 +593,7 @@ class PagedPlan:
         return row
 
     def _call(self, function, stream, *args):
-        if torch.cuda.current_device() == self.device.index:
+        if torch.cuda.current_device() == self.index:
             _check(function(self._handle, *args, stream))
         else:
             with torch.cuda.device(self.device):
