@@ -350,20 +350,39 @@ template <int DT> __device__ __forceinline__ uint32_t round_pair(float a, float 
   if constexpr (DT == DT_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
   else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
 }
-// V^T operands of 16 keys and D / 32 times 32 d by transposing reads: 16 lanes give the addresses of 4 keys x 16 d and get 4 keys of one d
-// each; the second four keys of a lane lie HI bytes further.  Its own wait stands in the block.
-template <int HI> __device__ __forceinline__ void read_keys_of_32d(const uint32_t (&a)[2], u32x4_t (&v)[2]) {
-  uint2 x[2], y[2];
-  asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %2, %4 offset:%6\n\t"
-               "ds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\t"
+// V^T operands of twice 16 keys (RB * 16 bytes apart, OFF bytes from a on) and N times 32 d by transposing reads: 16 lanes give the addresses of 4 keys
+// x 16 d and get 4 keys of one d each; the second four keys of a lane lie 8 rows further.  The wait stands in the block.
+template <int RB, int OFF> __device__ __forceinline__ void read_keys_of_32d(const uint32_t (&a)[4], u32x4_t (&v)[2][4]) {
+  uint2 x[16];
+  asm volatile("ds_read_b64_tr_b16 %0, %16 offset:%20\n\tds_read_b64_tr_b16 %1, %16 offset:%21\n\t"
+               "ds_read_b64_tr_b16 %2, %17 offset:%20\n\tds_read_b64_tr_b16 %3, %17 offset:%21\n\t"
+               "ds_read_b64_tr_b16 %4, %18 offset:%20\n\tds_read_b64_tr_b16 %5, %18 offset:%21\n\t"
+               "ds_read_b64_tr_b16 %6, %19 offset:%20\n\tds_read_b64_tr_b16 %7, %19 offset:%21\n\t"
+               "ds_read_b64_tr_b16 %8, %16 offset:%22\n\tds_read_b64_tr_b16 %9, %16 offset:%23\n\t"
+               "ds_read_b64_tr_b16 %10, %17 offset:%22\n\tds_read_b64_tr_b16 %11, %17 offset:%23\n\t"
+               "ds_read_b64_tr_b16 %12, %18 offset:%22\n\tds_read_b64_tr_b16 %13, %18 offset:%23\n\t"
+               "ds_read_b64_tr_b16 %14, %19 offset:%22\n\tds_read_b64_tr_b16 %15, %19 offset:%23\n\t"
                "s_waitcnt lgkmcnt(0)"
-               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(y[0]), "=&v"(y[1])
-               : "v"(a[0]), "v"(a[1]), "n"(HI)
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(x[8]),
+                 "=&v"(x[9]), "=&v"(x[10]), "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15])
+               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(OFF), "n"(OFF + 8 * RB), "n"(OFF + 16 * RB), "n"(OFF + 24 * RB)
                : "memory");
 #pragma unroll
-  for (int i = 0; i < 2; ++i) v[i] = u32x4_t{x[i].x, x[i].y, y[i].x, y[i].y};
+  for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = u32x4_t{x[2 * i].x, x[2 * i].y, x[2 * i + 1].x, x[2 * i + 1].y};
 }
-template <int HI> __device__ __forceinline__ void read_keys_of_32d(const uint32_t (&a)[4], u32x4_t (&v)[4]) { read_keys_of_d<HI>(a, v); }
+template <int RB, int OFF> __device__ __forceinline__ void read_keys_of_32d(const uint32_t (&a)[2], u32x4_t (&v)[2][2]) {
+  uint2 x[8];
+  asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%10\n\tds_read_b64_tr_b16 %1, %8 offset:%11\n\t"
+               "ds_read_b64_tr_b16 %2, %9 offset:%10\n\tds_read_b64_tr_b16 %3, %9 offset:%11\n\t"
+               "ds_read_b64_tr_b16 %4, %8 offset:%12\n\tds_read_b64_tr_b16 %5, %8 offset:%13\n\t"
+               "ds_read_b64_tr_b16 %6, %9 offset:%12\n\tds_read_b64_tr_b16 %7, %9 offset:%13\n\t"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+               : "v"(a[0]), "v"(a[1]), "n"(OFF), "n"(OFF + 8 * RB), "n"(OFF + 16 * RB), "n"(OFF + 24 * RB)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i / 2][i % 2] = u32x4_t{x[2 * i].x, x[2 * i].y, x[2 * i + 1].x, x[2 * i + 1].y};
+}
 
 // 16 bytes of LDS from each of N addresses, OFF bytes further, with their wait: at an LDS read of its own the compiler waits for every
 // asynchronous copy in flight.
@@ -461,14 +480,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) sacc[kt] = mfma32<DT>(kf[ks], qf[ks], sacc[kt]);
     }
-    u32x4_t va[4][DTL];                       // on their way while the products are worked on
+    u32x4_t va[2][2][DTL];                    // 16-key steps; on their way while the products are worked on
+    uint32_t at[DTL];
 #pragma unroll
-    for (int st = 0; st < 4; ++st) {
-      uint32_t at[DTL];
-#pragma unroll
-      for (int dt = 0; dt < DTL; ++dt) at[dt] = (vaddr + b * (2 * BUF) + st * 16 * RB) ^ (dt * 64);
-      read_keys_of_32d<8 * RB>(at, va[st]);
-    }
+    for (int dt = 0; dt < DTL; ++dt) at[dt] = (vaddr + b * (2 * BUF)) ^ (dt * 64);
+    read_keys_of_32d<RB, 0>(at, va[0]);
+    read_keys_of_32d<RB, 32 * RB>(at, va[1]);
     if (careful || !full) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
@@ -478,6 +495,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
           sacc[kt][i] = ((key <= qpos) & ((key >= qlo) | (key < v.sinks))) ? sacc[kt][i] : -INFINITY;
         }
     }
+    __builtin_amdgcn_s_setprio(1);
     float top = sacc[0][0];
 #pragma unroll
     for (int i = 1; i < 32; ++i) top = fmaxf(top, sacc[i >> 4][i & 15]);
@@ -506,11 +524,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       for (int dt = 0; dt < DTL; ++dt) {
         if constexpr (careful) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) va[st][dt][e] = finite_only<DT>(va[st][dt][e]);
+          for (int e = 0; e < 4; ++e) va[st >> 1][st & 1][dt][e] = finite_only<DT>(va[st >> 1][st & 1][dt][e]);
         }
-        oacc[dt] = mfma32<DT>(va[st][dt], pb, oacc[dt]);
+        oacc[dt] = mfma32<DT>(va[st >> 1][st & 1][dt], pb, oacc[dt]);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     if constexpr (careful) {
       for (int j = 0; j < kTileKeys; ++j) {
         const int key = k0 + j;

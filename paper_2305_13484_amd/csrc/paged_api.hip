@@ -158,6 +158,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
         longest = std::max<int64_t>(longest, end - skip);
       }
     }
+    std::stable_sort(items.begin(), items.end(), [](const PagedItem& a, const PagedItem& b) { return a.u1 > b.u1; });
     // The least share of steps, four at least, that makes no more blocks than `most`
     const int64_t all = steps * sh.n_kv_head;
     const int64_t most = std::min<int64_t>(kBlocks[kind][1], std::max<int64_t>(kBlocks[kind][0], all / 32));
