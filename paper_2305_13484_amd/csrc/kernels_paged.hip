@@ -668,7 +668,7 @@ __device__ __forceinline__ void copy_words_to_lds(const char* base, uint32_t off
                                            (__attribute__((address_space(3))) void*)l, 4, off, 0, 0, 0);
 }
 // Whether a sequence's weights are the streaming kernel's, or the tile kernel's.
-template <int DT> __device__ __forceinline__ bool few_rows(int rows) { return DT == DT_F32 || rows <= kRowTile; }
+__device__ __forceinline__ bool few_rows(int rows) { return rows <= kRowTile; }
 // New tokens [t0, t1) of a sequence see some of keys [k0, k1).
 __device__ __forceinline__ int first_token(const PagedSeq& s, int k0) { return max(0, k0 - (s.len - s.fresh)); }
 __device__ __forceinline__ int end_token(const PagedView& v, const PagedSeq& s, int k0, int k1) {
@@ -692,7 +692,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F3
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, n = lane & 15, kvh = blockIdx.y;
   const PagedSeq s = uniform_load(v.seqs + blockIdx.z);
-  if (!few_rows<DT>(s.fresh * v.group)) return;
+  if (!few_rows(s.fresh * v.group)) return;
   const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
   const int end = min(s.len, (int)(blockIdx.x + 1) * keys);
   int k0 = blockIdx.x * keys + wave * KT;
@@ -714,24 +714,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F3
     }
   };
   u32x4_t qf[KS];
-  float base[4];                                               // of rows r0 + 4g + r: lse in base 2, and the position
+  float base[4];                                               // of rows 4g + r: lse in base 2, and the position
   int at[4];
-  auto queries = [&](int r0, int r1) INLINED {
-    const int row = min(r0 + n, r1 - 1), token = quotient(row, v.by_group), head = kvh * v.group + row - token * v.group;
+  const int rows = s.fresh * v.group;
+  auto queries = [&]() INLINED {
+    const int row = min(n, rows - 1), token = quotient(row, v.by_group), head = kvh * v.group + row - token * v.group;
     const char* qr = q + (s.first + token) * qs + (size_t)head * RB + g * 16;
 #pragma unroll
     for (int i = 0; i < KS; ++i) qf[i] = *(const u32x4_t*)(qr + i * 64);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int rr = min(r0 + 4 * g + r, r1 - 1), tk = quotient(rr, v.by_group);
+      const int rr = min(4 * g + r, rows - 1), tk = quotient(rr, v.by_group);
       base[r] = lse[(size_t)(s.first + tk) * v.n_head + kvh * v.group + rr - tk * v.group] * kLog2e;
-      at[r] = r0 + 4 * g + r < r1 ? before + tk : -1;          // -1: no such row
+      at[r] = 4 * g + r < rows ? before + tk : -1;             // -1: no such row
     }
   };
-  const bool one = s.fresh * v.group <= kRowTile;              // all rows of queries at once: they stay in registers
   auto seen = [&](int k) INLINED { return first_token(s, k) < end_token(v, s, k, min(k + KT, s.len)); };      // by some new token
   if (seen(k0)) load(k0);
-  if (one && s.fresh > 0) queries(0, s.fresh * v.group);
+  if (rows > 0) queries();
   for (; k0 < end; k0 += 4 * KT) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -744,12 +744,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F3
     const bool writes = g < KG && mine < s.len, brought = mine >= before;
     const float old = writes && decay != 0.f && !brought ? *to : 0.f;
     if (k0 + 4 * KT < end && seen(k0 + 4 * KT)) load(k0 + 4 * KT);
-    const int k1 = min(k0 + KT, s.len), t0 = first_token(s, k0), t1 = end_token(v, s, k0, k1);
     float sum[KG];
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) sum[kg] = 0.f;
-    for (int r0 = one ? 0 : t0 * v.group; t0 < t1 && r0 < t1 * v.group; r0 += 16) {
-      if (!one) queries(r0, t1 * v.group);
+    if (seen(k0)) {
 #pragma unroll
       for (int kg = 0; kg < KG; ++kg) {
         f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
@@ -781,89 +779,127 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F3
   }
 }
 
-// Many rows of queries, 16-bit types.  A wave holds the K rows of 32 positions as operands and goes through the rows of queries that see any of
-// them; S[row][key] as above, a lane adds up 16 rows of its key.  The rows come to LDS by asynchronous copies, a ring of steps.
-//   SPLIT = false: grid = (blocks of 128 positions, n_kv, n_seq), the four waves share steps of 64 rows, three in the ring;
-//   SPLIT = true:  grid = (blocks of 32 positions, n_kv, n_seq), every wave has its own steps of 32 rows, each fourth one, two in the ring, and the
-//                  waves' sums are joined in their order: four times the blocks and a quarter of the steps, for four times the rows read.
+// Many rows of queries.  A wave holds the K rows of 32 positions as operands and goes through the rows of queries that see any of them; S[row][key]
+// as above, a lane adds up the rows of its key (fp32: two keys, of either 16-key group).  The rows come to LDS by asynchronous copies, a ring of steps.
+//   SPLIT = false: grid = (blocks of 128 positions, n_kv, n_seq), the four waves share steps of 64 rows (fp32: 32), three in the ring;
+//   SPLIT = true:  grid = (blocks of 32 positions, n_kv, n_seq), every wave has its own steps of half as many rows, each fourth one, two in the ring,
+//                  and the waves' sums are joined in their order: four times the blocks and a quarter of the rows each, for four times the rows read.
 // Split where blocks of 128 positions are 128 or fewer, one for two compute units (us, shared -> split, d = 128: 64 blocks, 8 heads, 100 new tokens of
 // 1000 rows 6.2 -> 5.0, 32 heads on 8, 1000 of 1000 64 -> 27; 128 blocks, 200 of 2000 18.8 -> 12.4, 2000 of 2000 122 -> 90; 192 blocks, 16 heads,
 // 1500 of 1500 28.1 -> 24.2, 500 of 1500 13.4 -> 16.2; 256 blocks, 32 heads, 1000 of 1000 20.9 -> 26.9).
-// Vector instructions bound it: an exponential takes 16 cycles of a wave, its product's share 8, and the sum and the scaling 4 each.
+// 16-bit types: vector instructions bound it, an exponential takes 16 cycles of a wave, its product's share 8, the sum and the scaling 4 each.  fp32:
+// the products (16 x 16 x 4).
+
+// The rows of a block's, or of a wave's, steps and their lse.
+template <int RB, int ROWS, int WAVES, int RING> struct QueryRing {
+  static constexpr int SEG = RB / 16, RPC = 64 / SEG, NC = ROWS / WAVES / RPC;      // pieces of a row, rows of a copy, copies of a wave per step
+  char* rows;                     // LDS: [RING][ROWS * RB], 16-byte pieces permuted by row
+  float* lse;                     // LDS: [RING][64], of every wave for itself
+  const char* q;
+  const float* from_lse;
+  int64_t qs;
+  int b0, b1, wave, lane, kvh;    // rows [b0, b1) of the sequence; the wave among those that share the steps
+  uint32_t at[NC], lse_at;        // offsets of the lane's pieces of a step from the step's first token on
+  bool alike;                     // steps begin with a token: the same offsets, but for the last
+  static __device__ __forceinline__ int swizzle(int row) { return SEG == 8 ? (row >> 1) & 7 : row & 15; }
+  __device__ __forceinline__ void start(const PagedView& v, const PagedSeq& s, const char* q_, int64_t qs_, const float* lse_, int u) {
+    q = q_ + s.first * qs_ + (size_t)kvh * v.group * RB;
+    from_lse = lse_ + (size_t)s.first * v.n_head + kvh * v.group;
+    qs = qs_;
+    alike = ROWS % v.group == 0;
+    offsets(v, b0 + u * ROWS);
+  }
+  __device__ __forceinline__ void offsets(const PagedView& v, int r0) {
+    const int ta = quotient(r0, v.by_group);                        // offsets from there fit 32 bits
+    auto from = [&](int r, int per_token, int per_head) INLINED {   // row b1 - 1 again behind the last
+      const int row = min(r0 + r, b1 - 1), token = quotient(row, v.by_group);
+      return (uint32_t)((token - ta) * per_token + (row - token * v.group) * per_head);
+    };
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int r = (wave * NC + j) * RPC + lane / SEG;
+      at[j] = from(r, (int)qs, RB) + ((lane % SEG) ^ swizzle(r)) * 16;
+    }
+    lse_at = from(lane, v.n_head * 4, 4);
+  }
+  __device__ __forceinline__ void issue(const PagedView& v, int u, int slot) {
+    const int r0 = b0 + u * ROWS, ta = quotient(r0, v.by_group);
+    if (!alike || r0 + 64 > b1) offsets(v, r0);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) copy_to_lds(q + ta * qs, at[j], (u32x4_t*)(rows + slot * (ROWS * RB) + (wave * NC + j) * 1024));
+    copy_words_to_lds((const char*)(from_lse + (size_t)ta * v.n_head), lse_at, lse + slot * 64);
+  }
+};
+
 template <int DT, int D, bool SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_weights_tile_kernel(
     PagedView v, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc, const float* __restrict__ lse, float decay,
     float* __restrict__ w, int64_t ws) {
-  constexpr int RB = D * 2, KS = D / 16, SEG = D / 8, RPC = 64 / SEG;
-  constexpr int ROWS = SPLIT ? 32 : 64, X = ROWS / 32, RING = SPLIT ? 2 : 3, KEYS = SPLIT ? 32 : 128;
-  constexpr int NC = ROWS / (SPLIT ? 1 : 4) / RPC;                  // copies of a wave per step
+  constexpr bool F32 = DT == DT_F32;
+  constexpr int RB = D * (F32 ? 4 : 2);
+  constexpr int KG = F32 ? 2 : 1, KL = 32 / KG, KS = RB / (F32 ? 64 : 32);      // keys of a lane, lanes of a key group, operands of a row
+  constexpr int ROWS = (F32 ? 32 : 64) / (SPLIT ? 2 : 1), X = ROWS / KL, RING = SPLIT ? 2 : 3, KEYS = SPLIT ? 32 : 128;
+  typedef QueryRing<RB, ROWS, SPLIT ? 1 : 4, RING> Ring;
+  constexpr int NC = Ring::NC;
   __shared__ __attribute__((aligned(1024))) char rows_lds[SPLIT ? 4 : 1][RING][ROWS * RB];
   __shared__ __attribute__((aligned(1024))) float lse_lds[4][RING][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = lane >> 5, n = lane & 31, kvh = blockIdx.y;
+  const int h = lane / KL, n = lane % KL, kvh = blockIdx.y;          // part of a row's operand, key of the group
   const PagedSeq s = uniform_load(v.seqs + blockIdx.z);
-  if (few_rows<DT>(s.fresh * v.group)) return;
+  if (few_rows(s.fresh * v.group)) return;
   const int kb0 = blockIdx.x * KEYS;
   if (kb0 >= s.len) return;
   const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
-  const int k0 = SPLIT ? kb0 : kb0 + wave * 32, key = k0 + n;
+  const int k0 = SPLIT ? kb0 : kb0 + wave * 32;
   // rows that see some key of the block: [b0, b1); that see the lane's key: [lo, lo + number)
   const int b0 = first_token(s, kb0) * v.group, b1 = end_token(v, s, kb0, min(kb0 + KEYS, s.len)) * v.group;
-  const int lo = first_token(s, key) * v.group;
-  const uint32_t number = key < s.len ? (uint32_t)max(0, end_token(v, s, key, key + 1) * v.group - lo) : 0;
+  int lo[KG];
+  uint32_t number[KG];
+#pragma unroll
+  for (int kg = 0; kg < KG; ++kg) {
+    const int key = k0 + kg * KL + n;
+    lo[kg] = first_token(s, key) * v.group;
+    number[kg] = key < s.len ? (uint32_t)max(0, end_token(v, s, key, key + 1) * v.group - lo[kg]) : 0;
+  }
   // ... of all of the wave's keys, of some of them
   const int oldest = max(k0, min(v.sinks, k0 + 31));                // the wave's key that drops out of the window first
   const int all0 = first_token(s, k0 + 31) * v.group, all1 = k0 + 32 > s.len ? 0 : end_token(v, s, oldest, oldest + 1) * v.group;
   const int any0 = first_token(s, k0) * v.group, any1 = k0 < s.len ? end_token(v, s, k0, min(k0 + 32, s.len)) * v.group : 0;
   const float c = v.scale * kLog2e;
 
-  u32x4_t kf[KS];
+  u32x4_t kf[KG][KS];
   {
-    const int pl = min(k0, last16), ph = min(k0 + 16, last16), p = n & 16 ? ph : pl;
+    const int pl = min(k0, last16), ph = min(k0 + 16, last16);
     const uint32_t rl = cache_row(v, s, kvh, pl), rh = cache_row(v, s, kvh, ph);
-    const char* kr = kc + (size_t)((n & 16 ? rh : rl) + min(n & 15, s.len - 1 - p)) * RB + h * 16;
 #pragma unroll
-    for (int i = 0; i < KS; ++i) kf[i] = *(const u32x4_t*)(kr + i * 32);
-  }
-  auto swizzle = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
-  // offsets of the lane's pieces of a step from the step's first row on; row b1 - 1 again behind the last
-  uint32_t at[NC], lse_at;
-  auto offsets = [&](int r0) INLINED {
-    const int ta = quotient(r0, v.by_group);                        // the step's first token: offsets from there fit 32 bits
-    auto from = [&](int r, int per_token, int per_head) INLINED {
-      const int row = min(r0 + r, b1 - 1), token = quotient(row, v.by_group);
-      return (uint32_t)((token - ta) * per_token + (row - token * v.group) * per_head);
-    };
+    for (int kg = 0; kg < KG; ++kg) {
+      const bool high = F32 ? kg == 1 : (n & 16) != 0;
+      const char* kr = kc + (size_t)((high ? rh : rl) + min(n & 15, s.len - 1 - (high ? ph : pl))) * RB + h * 16;
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int r = ((SPLIT ? 0 : wave * NC) + j) * RPC + lane / SEG;
-      at[j] = from(r, (int)qs, RB) + ((lane % SEG) ^ swizzle(r)) * 16;
+      for (int i = 0; i < KS; ++i) kf[kg][i] = *(const u32x4_t*)(kr + i * (F32 ? 64 : 32));
     }
-    lse_at = from(lane, v.n_head * 4, 4);
-  };
-  const bool alike = ROWS % v.group == 0;                            // steps begin with a token: the same offsets, but for the last
-  auto issue = [&](int u, int slot) INLINED {
-    const int r0 = b0 + u * ROWS, ta = quotient(r0, v.by_group);
-    if (!alike || r0 + 64 > b1) offsets(r0);
-    const char* qb = q + (s.first + ta) * qs + (size_t)kvh * v.group * RB;
-#pragma unroll
-    for (int j = 0; j < NC; ++j)
-      copy_to_lds(qb, at[j], (u32x4_t*)(rows_lds[SPLIT ? wave : 0][slot] + ((SPLIT ? 0 : wave * NC) + j) * 1024));
-    copy_words_to_lds((const char*)(lse + (size_t)(s.first + ta) * v.n_head + kvh * v.group), lse_at, lse_lds[wave][slot]);
-  };
+  }
+  Ring ring;
+  ring.rows = rows_lds[SPLIT ? wave : 0][0];
+  ring.lse = lse_lds[wave][0];
+  ring.b0 = b0;
+  ring.b1 = b1;
+  ring.wave = SPLIT ? 0 : wave;
+  ring.lane = lane;
+  ring.kvh = kvh;
   const uint32_t qaddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&rows_lds[SPLIT ? wave : 0][0][0] +
-                         (uint32_t)(n * RB + (h ^ swizzle(n)) * 16);
+                         (uint32_t)(n * RB + (h ^ Ring::swizzle(n)) * 16);
   const uint32_t laddr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)&lse_lds[wave][0][0];
   const int steps = b1 > b0 ? (b1 - b0 + ROWS - 1) / ROWS : 0;
   constexpr int BY = SPLIT ? 4 : 1;
   const int first = SPLIT ? wave : 0;
-  float sum[X];
+  float sum[KG][2];
 #pragma unroll
-  for (int x = 0; x < X; ++x) sum[x] = 0.f;
-  if (first < steps) offsets(b0 + first * ROWS);
+  for (int kg = 0; kg < KG; ++kg) sum[kg][0] = sum[kg][1] = 0.f;
+  if (first < steps) ring.start(v, s, q, qs, lse, first);
 #pragma unroll
   for (int i = 0; i < RING - 1; ++i)
-    if (first + i * BY < steps) issue(first + i * BY, i);
+    if (first + i * BY < steps) ring.issue(v, first + i * BY, i);
   for (int u = first, slot = 0; u < steps; u += BY, slot = slot + 1 == RING ? 0 : slot + 1) {
     const int ahead = u + (RING - 1) * BY;
     if constexpr (SPLIT) {
@@ -872,7 +908,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     } else {
       copies_barrier<(NC + 1) * (RING - 2)>(ahead - 1 >= steps);
     }
-    if (ahead < steps) issue(ahead, slot == 0 ? RING - 1 : slot - 1);
+    if (ahead < steps) ring.issue(v, ahead, slot == 0 ? RING - 1 : slot - 1);
     const int r0 = b0 + u * ROWS, r1 = min(r0 + ROWS, b1);
     if (r1 <= any0 || r0 >= any1) continue;
     // lse of the step's rows in base 2, in place
@@ -880,51 +916,90 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     float mine;
     asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(mine) : "v"(la + lane * 4) : "memory");
     asm volatile("ds_write_b32 %0, %1" ::"v"(la + lane * 4), "v"(mine * kLog2e) : "memory");
-    f32x16_t sacc[X];
-    uint32_t qa[KS], pa[4];
+    uint32_t qa[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qa[ks] = (qaddr + slot * (ROWS * RB)) ^ (ks * 32);
+    for (int i = 0; i < KS; ++i) qa[i] = (qaddr + slot * (ROWS * RB)) ^ (i * (F32 ? 64 : 32));
+    const bool whole = r0 >= all0 && r0 + ROWS <= min(all1, b1);
+    if constexpr (F32) {
+      u32x4_t qf[X][KS], bits[X];             // lse of the lane's rows 16 x + 4 h + ..
+      f32x4_t sacc[X][KG];
+      read_pieces<0>(qa, qf[0]);
+      if constexpr (X > 1) read_pieces<16 * RB>(qa, qf[X - 1]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) pa[i] = la + i * 32 + h * 16;
-    u32x4_t bits[X][4];                       // lse of the lane's rows 8 i + 4 h + .. of each product
-    auto product = [&](auto x_) INLINED {
-      constexpr int x = decltype(x_)::value;
-      u32x4_t qf[KS];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sacc[x][i] = 0.f;
-      read_pieces<x * 32 * RB>(qa, qf);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sacc[x] = mfma32<DT>(qf[ks], kf[ks], sacc[x]);
-    };
-    product(std::integral_constant<int, 0>{});
-    if constexpr (X > 1) product(std::integral_constant<int, X - 1>{});
-    read_pieces<0>(pa, bits[0]);
-    if constexpr (X > 1) read_pieces<128>(pa, bits[X - 1]);
-    auto add = [&](auto whole) INLINED {
-      const int r = r0 + 4 * h - lo;
+      for (int x = 0; x < X; ++x)
+        asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(bits[x]) : "v"(la + x * 64 + h * 16) : "memory");
 #pragma unroll
       for (int x = 0; x < X; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float p = fmaf(sacc[x][i], c, -__uint_as_float(bits[x][i / 4][i % 4]));
-          if constexpr (!decltype(whole)::value) p = (uint32_t)(r + x * 32 + 8 * (i / 4) + i % 4) < number ? p : -INFINITY;
-          sum[x] += __builtin_amdgcn_exp2f(p);
-        }
-    };
-    if (r0 >= all0 && r0 + ROWS <= min(all1, b1)) add(std::true_type{});
-    else add(std::false_type{});
+        for (int kg = 0; kg < KG; ++kg) sacc[x][kg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int x = 0; x < X; ++x)
+#pragma unroll
+            for (int kg = 0; kg < KG; ++kg)
+              sacc[x][kg] = mfma_f32(__uint_as_float(qf[x][i][e]), __uint_as_float(kf[kg][i][e]), sacc[x][kg]);
+#pragma unroll
+      for (int x = 0; x < X; ++x)
+#pragma unroll
+        for (int kg = 0; kg < KG; ++kg)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = fmaf(sacc[x][kg][e], c, -__uint_as_float(bits[x][e]));
+            const bool seen = (uint32_t)(r0 + x * 16 + 4 * h + e - lo[kg]) < number[kg];
+            sum[kg][x & 1] += __builtin_amdgcn_exp2f(seen ? p : -INFINITY);
+          }
+    } else {
+      f32x16_t sacc[X];
+      uint32_t pa[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pa[i] = la + i * 32 + h * 16;
+      u32x4_t bits[X][4];                     // lse of the lane's rows 8 i + 4 h + .. of each product
+      auto product = [&](auto x_) INLINED {
+        constexpr int x = decltype(x_)::value;
+        u32x4_t qf[KS];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sacc[x][i] = 0.f;
+        read_pieces<x * 32 * RB>(qa, qf);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sacc[x] = mfma32<DT>(qf[ks], kf[0][ks], sacc[x]);
+      };
+      product(std::integral_constant<int, 0>{});
+      if constexpr (X > 1) product(std::integral_constant<int, X - 1>{});
+      read_pieces<0>(pa, bits[0]);
+      if constexpr (X > 1) read_pieces<128>(pa, bits[X - 1]);
+      auto add = [&](auto all) INLINED {
+        const int r = r0 + 4 * h - lo[0];
+#pragma unroll
+        for (int x = 0; x < X; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float p = fmaf(sacc[x][i], c, -__uint_as_float(bits[x][i / 4][i % 4]));
+            if constexpr (!decltype(all)::value) p = (uint32_t)(r + x * 32 + 8 * (i / 4) + i % 4) < number[0] ? p : -INFINITY;
+            sum[0][x] += __builtin_amdgcn_exp2f(p);
+          }
+      };
+      if (whole) add(std::true_type{});
+      else add(std::false_type{});
+    }
   }
-  float t = sum[0];
-  if constexpr (X > 1) t += sum[X - 1];
-  t = sum_partner<32>(t);
+  // lane `key` of 32: the sum of key k0 + key
+  float t = sum_partner<32>(sum[0][0] + sum[0][1]);
+  if constexpr (F32) {
+    const float t0 = sum_partner<16>(t), t1 = sum_partner<16>(sum_partner<32>(sum[KG - 1][0] + sum[KG - 1][1]));
+    t = lane < 16 ? t0 : t1;
+  }
   if constexpr (SPLIT) {
     __shared__ float sums[4][32];
-    if (h == 0) sums[wave][n] = t;
+    if (lane < 32) sums[wave][lane] = t;
     __syncthreads();
     if (wave > 0) return;
-    t = (sums[0][n] + sums[1][n]) + (sums[2][n] + sums[3][n]);
+    t = lane < 32 ? (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]) : 0.f;
   }
-  if (h == 0 && key < s.len) {
+  const int key = k0 + lane;
+  if (lane < 32 && key < s.len) {
     float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + key;
     *to = new_weight(t, decay != 0.f && key < before ? *to : 0.f, decay, key >= before);
   }
@@ -1166,8 +1241,7 @@ hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t q
     const int keys = few_blocks ? 256 : 512;
     if (few) paged_weights_rows_kernel<DT, D><<<dim3((v.longest + keys - 1) / keys, v.n_kv, v.n_seq), 256, 0, st>>>(
         v, (const char*)q, qb, (const char*)kc, lse, decay, w, ws, keys);
-    if constexpr (DT != DT_F32)
-      if (many) {
+    if (many) {
         auto launch = [&](auto split) {
           constexpr bool SPLIT = decltype(split)::value;
           constexpr int KEYS = SPLIT ? 32 : 128;

@@ -63,7 +63,7 @@ struct Lists {
   size_t pm = 0, po = 0, total = 0;                        // partial results, behind the lists
   int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_tiles = 0, n_merges = 0;
   int most_parts = 0, most_rows = 0;                       // of a merge
-  bool few = false, many = false;                          // sequences of up to 16 rows per key head (of fp32: all), of more,
+  bool few = false, many = false;                          // sequences of up to 16 rows per key head, of more,
   int64_t row_blocks = 0, tile_blocks = 0;                 // and their blocks of 512, of 128 positions of a key head
   bool shared = false, shared_new = false;                 // a page twice in use; one that new tokens go to
 };
@@ -71,6 +71,7 @@ struct Lists {
 // Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long: two of either are at work
 // on a compute unit.
 constexpr int kBlocks[2][2] = {{1024, 2048}, {512, 512}};
+constexpr int kWhole[2] = {16, 8};
 
 int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const int32_t* len, const int32_t* table, int stride, Lists* L) {
   auto bad = [](const std::string& m) { return fail_call(FLOVER_E_INVAL, m); };
@@ -106,7 +107,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   for (int i = 0; i < n_seq; ++i) {
     const int need = (len[i] + sh.page_size - 1) / sh.page_size, fresh = len[i] - new_len[i];
     seqs[i] = {first, new_len[i], len[i], (int)pages.size()};
-    if (sh.dtype == FLOVER_F32 || (int64_t)new_len[i] * group <= flk::kRowTile) {
+    if ((int64_t)new_len[i] * group <= flk::kRowTile) {
       L->few = true;
       L->row_blocks += ((int64_t)len[i] + 511) / 512 * sh.n_kv_head;
     } else {
@@ -162,7 +163,8 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
     // The least share of steps, four at least, that makes no more blocks than `most`
     const int64_t all = steps * sh.n_kv_head;
     const int64_t most = std::min<int64_t>(kBlocks[kind][1], std::max<int64_t>(kBlocks[kind][0], all / 32));
-    int64_t share = std::max<int64_t>(4, (all + most - 1) / most);
+    // ... and none at all where no row has more than kWhole steps: the launch that joins parts costs more than they save
+    int64_t share = std::max<int64_t>(longest <= kWhole[kind] ? longest : 4, (all + most - 1) / most);
     for (int64_t low = share, high = std::max<int64_t>(share, longest); low < high; share = high) {
       const int64_t mid = (low + high) / 2;
       int64_t blocks = 0;
