@@ -354,7 +354,8 @@ typedef struct flover_paged_shape {
   int32_t dtype;                         /* FLOVER_F32 | FLOVER_F16 | FLOVER_BF16: queries, cache, output */
   int32_t n_head, n_kv_head, head_dim;   /* n_head a multiple of n_kv_head; head_dim in {64,128} */
   int32_t page_size, n_pages;            /* page_size a multiple of 16, or any size if no sequence has a second page;
-                                            n_pages * n_kv_head * page_size < 2^31 */
+                                            n_pages * n_kv_head * page_size < 2^31; a sequence has
+                                            fewer than 2^30 rows */
   int32_t window, sinks;                 /* window > 0: position p sees its last `window` positions, itself among them, and the first
                                             `sinks`; window == 0: all up to itself (sinks is not read then) */
 } flover_paged_shape;
@@ -383,7 +384,7 @@ int32_t flover_k_paged_plan_set(flover_paged_plan* plan, int32_t n_seq, const in
 int32_t flover_k_paged_plan_destroy(flover_paged_plan* plan);   /* waits for the plan's last copy; NULL is a no-op */
 
 /* Rows of the new tokens to their places: k, v [device][T] rows of [n_kv_head][head_dim], k_stride / v_stride elements apart
- * (a multiple of 16 bytes, at most 64 MB; views into a packed q|k|v row are fine), 16-byte aligned.  Refused (INVAL) where two sequences of
+ * (a multiple of 16 bytes, at most 16 MB; views into a packed q|k|v row are fine), 16-byte aligned.  Refused (INVAL) where two sequences of
  * the plan share a page that new tokens go to. */
 int32_t flover_k_paged_append(const flover_paged_plan* plan, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                               void* kcache, void* vcache, void* stream);

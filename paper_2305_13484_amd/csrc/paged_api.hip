@@ -84,6 +84,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   for (int i = 0; i < n_seq; ++i) {
     const std::string at = " of sequence " + std::to_string(i);
     if (new_len[i] < 0 || len[i] < new_len[i]) return bad("new_len / len" + at);
+    if (len[i] >= 1 << 30) return bad("2^30 rows or more" + at);
     const int64_t need = ((int64_t)len[i] + sh.page_size - 1) / sh.page_size;
     if (need > stride) return bad("rows beyond the page table" + at);
     if (need > 1 && sh.page_size % 16) return bad("second page of a size that is no multiple of 16" + at);
@@ -93,7 +94,9 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
     tokens += new_len[i];
     L->longest = std::max(L->longest, len[i]);
   }
-  if (tokens * sh.n_head >= 2147483648LL) return bad("too many new tokens");
+  // what the kernels count in 32 bits: rows of queries, and the threads of a launch
+  if (tokens * sh.n_head >= 2147483648LL || tokens * sh.n_kv_head * (sh.head_dim * esize(sh.dtype) / 16) >= 4294967296LL)
+    return bad("too many new tokens");
   L->n_seq = n_seq;
   L->tokens = (int)tokens;
 
@@ -202,7 +205,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
       if (partial >= 2147483648LL) return bad("too many partial results");
     }
   }
-  if ((int64_t)(rows.size() + tiles.size() + merges.size()) * sh.n_kv_head >= 2147483648LL) return bad("too much work for one launch");
+  if ((int64_t)std::max({rows.size(), tiles.size(), merges.size()}) * sh.n_kv_head >= 1 << 24) return bad("too much work for one launch");
   L->n_rows = (int)rows.size();
   L->n_tiles = (int)tiles.size();
   L->n_merges = (int)merges.size();
@@ -264,8 +267,9 @@ struct flover_paged_plan {
     v.page_size = shape.page_size;
     v.by_group = flk::divisor(v.group);
     v.by_page = flk::divisor(v.page_size);
-    v.window = shape.window;
-    v.sinks = shape.window > 0 ? shape.sinks : 0;
+    const bool bounded = shape.window > 0 && shape.window < lists.longest;      // otherwise every token sees all up to itself
+    v.window = bounded ? shape.window : 0;
+    v.sinks = bounded ? shape.sinks : 0;
     v.scale = 1.0f / std::sqrt((float)shape.head_dim);
     return v;
   }
@@ -296,8 +300,8 @@ int ready(const flover_paged_plan* p, hipStream_t st) {
 // Checks of a row tensor [tokens] of `width` elements, `stride` apart.
 int check_rows(const flover_paged_plan* p, const void* x, int64_t stride, int64_t width, const char* name) {
   if (!x) return fail_call(FLOVER_E_INVAL, std::string("null ") + name);
-  if (!aligned16(x) || stride < width || stride % (16 / esize(p->shape.dtype)) || stride > (int64_t)(1 << 26) / esize(p->shape.dtype))
-    return fail_call(FLOVER_E_INVAL, std::string(name) + ": rows on 16 bytes, a stride of at least the row and at most 64 MB");
+  if (!aligned16(x) || stride < width || stride % (16 / esize(p->shape.dtype)) || stride > (int64_t)(1 << 24) / esize(p->shape.dtype))
+    return fail_call(FLOVER_E_INVAL, std::string(name) + ": rows on 16 bytes, a stride of at least the row and at most 16 MB");
   return FLOVER_OK;
 }
 int check_plan(const flover_paged_plan* p) {

@@ -60,6 +60,16 @@ def test_attention_in_a_window(fl, dtype, d, window, sinks):
     check_attention(fl, Case(dtype, 8, 4, d, 32, new, lens, window, sinks, seed=window))
 
 
+def test_a_window_longer_than_any_sequence_is_none(fl):
+    c = Case(BF, 8, 2, 64, 16, [1, 40], [300, 90], seed=2)
+    q, k, v, lse = c.q.cuda(), c.k.cuda(), c.v.cuda(), c.attention()[1].float().cuda()
+    w = torch.zeros(2, 2, 300, device="cuda")
+    plans = [c.plan(fl), c.plan(fl, window=300, sinks=7), c.plan(fl, window=2 ** 31 - 1, sinks=2 ** 31 - 1)]
+    outs = [(fl.k_paged_attention(p, q, k, v), fl.k_paged_weights(p, q, k, lse, w.clone())) for p in plans]
+    for a, b in outs[1:]:
+        assert torch.equal(a, outs[0][0]) and torch.equal(b, outs[0][1])
+
+
 @pytest.mark.parametrize("dtype", [BF, HF, F32])
 @pytest.mark.parametrize("page,lens", [(16, [160]), (700, [700, 33, 1]), (333, [100, 333]), (256, [1000, 257]), (112, [500, 113])])
 def test_page_sizes(fl, dtype, page, lens):
@@ -183,6 +193,14 @@ def test_weights_in_a_window(fl, dtype, d, window, sinks):
     check_weights(fl, Case(dtype, 8, 4, d, 32, [1, 1, 50, 129, 5, 300], [1, 300, 260, 129, 420, 700], window, sinks, seed=window), 0.0)
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (HF, 64), (F32, 128), (F32, 64)])
+def test_weights_of_many_blocks(fl, dtype, d):
+    """More than 128 blocks of 128 positions (the waves of a block share the rows), more than 1024 of 512 (longer blocks of the streaming kernel)."""
+    check_weights(fl, Case(dtype, 16, 8, d, 64, [70, 130, 0], [1500, 1000, 30], seed=d), 0.9)
+    check_weights(fl, Case(dtype, 6, 6, d, 16, [90, 200], [1700, 1200], 300, 40, seed=d), 0.9)
+    check_weights(fl, Case(dtype, 8, 8, d, 16, [1] * 132, [5 + 3 * i for i in range(132)], seed=d), 0.9)
+
+
 def test_weights_without_decay_overwrite_whatever_was_there(fl):
     c = Case(BF, 4, 2, 64, 16, [1, 2], [40, 30], seed=1)
     lse = c.attention()[1].float().cuda()
@@ -228,6 +246,22 @@ def test_evict(fl, dtype, n_kv, d, page, budget, first, recent):
     g = torch.Generator().manual_seed(budget)
     w = torch.exp(2 * torch.randn((len(lens), n_kv, max(lens)), generator=g))
     check_evict(fl, c, w, budget, first, recent, in_place=budget % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_evict_many_sequences(fl, dtype):
+    """Enough sequences for the wider pieces of a row."""
+    lens = [20 + 11 * i for i in range(40)]
+    c = Case(dtype, 4, 4, 128, 32, [0] * len(lens), lens, seed=3)
+    check_evict(fl, c, torch.rand((len(lens), 4, max(lens)), generator=torch.Generator().manual_seed(3)), 150, 3, 40, in_place=False)
+
+
+def test_evict_from_a_long_sequence(fl):
+    """More positions than a block holds in LDS, ties across that border."""
+    c = Case(HF, 1, 1, 64, 256, [0, 0], [21000, 19000], seed=3)
+    w = torch.rand((2, 1, 21000), generator=torch.Generator().manual_seed(3))
+    w[1] = (w[1] * 40).floor()
+    check_evict(fl, c, w, 9000, 3, 40, in_place=True)
 
 
 @pytest.mark.parametrize("in_place", [False, True])

@@ -56,11 +56,19 @@ def test_entries_behind_the_last_page_are_not_read_and_empty_lists_are_fine():
     assert plan_bytes(shape(), np.zeros(0), np.zeros(0), np.zeros((0, 0)))[0] == 0
 
 
+def test_lists_that_no_launch_could_take():
+    table = [list(range(1 << 15))]
+    rc, _, text = plan_bytes(shape(page_size=1 << 15, n_pages=1 << 15, n_kv_head=1), [0], [1 << 30], table)
+    assert rc == -1 and "2^30" in text
+    rc, _, text = plan_bytes(shape(page_size=1 << 20, n_pages=1 << 10, n_kv_head=1), [1 << 29], [1 << 29], [list(range(1 << 9))])
+    assert rc == -1 and "too many new tokens" in text
+
+
 def test_room_grows_with_keys_shared_out():
-    """One long sequence: partial results of 16 rows per part and key head; many even ones: none."""
+    """One long sequence: partial results of 16 rows per part and key head; many even ones: none, a work item of 80 bytes and the lists."""
     long = plan_bytes(shape(n_pages=4096), [1], [16 * 4000], [list(range(4000))])[1]
     many = plan_bytes(shape(n_pages=4096), [1] * 2000, [16] * 2000, [[i] for i in range(2000)])[1]
-    assert long > 2 * 16 * 130 * 4 * 8 and many < 2000 * 100
+    assert long > 2 * 16 * 130 * 4 * 8 and many < 2000 * 128
 
 
 def test_binding_checks_lists_before_the_device():
