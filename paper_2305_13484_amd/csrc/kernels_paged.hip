@@ -781,8 +781,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F3
 
 // Many rows of queries.  A wave holds the K rows of 32 positions as operands and goes through the rows of queries that see any of them; S[row][key]
 // as above, a lane adds up the rows of its key (fp32: two keys, of either 16-key group).  The rows come to LDS by asynchronous copies, a ring of steps.
-//   SPLIT = false: grid = (blocks of 128 positions, n_kv, n_seq), the four waves share steps of 64 rows (fp32: 32), three in the ring;
-//   SPLIT = true:  grid = (blocks of 32 positions, n_kv, n_seq), every wave has its own steps of half as many rows, each fourth one, two in the ring,
+//   SPLIT = false: grid = n_kv x entries of 128 positions, the four waves share steps of 64 rows (fp32: 32), three in the ring;
+//   SPLIT = true:  grid = (n_kv x entries, 4), 32 positions, every wave has its own steps of half as many rows, each fourth one, two in the ring,
 //                  and the waves' sums are joined in their order: four times the blocks and a quarter of the rows each, for four times the rows read.
 // Split where blocks of 128 positions are 128 or fewer, one for two compute units (us, shared -> split, d = 128: 64 blocks, 8 heads, 100 new tokens of
 // 1000 rows 6.2 -> 5.0, 32 heads on 8, 1000 of 1000 64 -> 27; 128 blocks, 200 of 2000 18.8 -> 12.4, 2000 of 2000 122 -> 90; 192 blocks, 16 heads,
@@ -833,21 +833,21 @@ template <int RB, int ROWS, int WAVES, int RING> struct QueryRing {
 
 template <int DT, int D, bool SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_weights_tile_kernel(
-    PagedView v, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc, const float* __restrict__ lse, float decay,
-    float* __restrict__ w, int64_t ws) {
+    PagedView v, const PagedKeys* __restrict__ blocks, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc,
+    const float* __restrict__ lse, float decay, float* __restrict__ w, int64_t ws) {
   constexpr bool F32 = DT == DT_F32;
   constexpr int RB = D * (F32 ? 4 : 2);
   constexpr int KG = F32 ? 2 : 1, KL = 32 / KG, KS = RB / (F32 ? 64 : 32);      // keys of a lane, lanes of a key group, operands of a row
-  constexpr int ROWS = (F32 ? 32 : 64) / (SPLIT ? 2 : 1), X = ROWS / KL, RING = SPLIT ? 2 : 3, KEYS = SPLIT ? 32 : 128;
+  constexpr int ROWS = (F32 ? 32 : 64) / (SPLIT ? 2 : 1), X = ROWS / KL, RING = SPLIT ? 2 : 3, KEYS = SPLIT ? 32 : kWeighKeys;
   typedef QueryRing<RB, ROWS, SPLIT ? 1 : 4, RING> Ring;
   constexpr int NC = Ring::NC;
   __shared__ __attribute__((aligned(1024))) char rows_lds[SPLIT ? 4 : 1][RING][ROWS * RB];
   __shared__ __attribute__((aligned(1024))) float lse_lds[4][RING][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = lane / KL, n = lane % KL, kvh = blockIdx.y;          // part of a row's operand, key of the group
-  const PagedSeq s = uniform_load(v.seqs + blockIdx.z);
-  if (few_rows(s.fresh * v.group)) return;
-  const int kb0 = blockIdx.x * KEYS;
+  const int h = lane / KL, n = lane % KL, kvh = blockIdx.x % v.n_kv;  // part of a row's operand, key of the group
+  const PagedKeys block = uniform_load(blocks + blockIdx.x / v.n_kv);
+  const PagedSeq s = uniform_load(v.seqs + block.seq);
+  const int kb0 = block.key0 + blockIdx.y * KEYS;
   if (kb0 >= s.len) return;
   const int before = s.len - s.fresh, last16 = (s.len - 1) & ~15;
   const int k0 = SPLIT ? kb0 : kb0 + wave * 32;
@@ -970,6 +970,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       if constexpr (X > 1) product(std::integral_constant<int, X - 1>{});
       read_pieces<0>(pa, bits[0]);
       if constexpr (X > 1) read_pieces<128>(pa, bits[X - 1]);
+      __builtin_amdgcn_s_setprio(1);
       auto add = [&](auto all) INLINED {
         const int r = r0 + 4 * h - lo[0];
 #pragma unroll
@@ -983,6 +984,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
       };
       if (whole) add(std::true_type{});
       else add(std::false_type{});
+      __builtin_amdgcn_s_setprio(0);
     }
   }
   // lane `key` of 32: the sum of key k0 + key
@@ -1000,7 +1002,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   }
   const int key = k0 + lane;
   if (lane < 32 && key < s.len) {
-    float* to = w + ((int64_t)blockIdx.z * v.n_kv + kvh) * ws + key;
+    float* to = w + ((int64_t)block.seq * v.n_kv + kvh) * ws + key;
     *to = new_weight(t, decay != 0.f && key < before ? *to : 0.f, decay, key >= before);
   }
 }
@@ -1232,7 +1234,7 @@ hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows,
 }
 
 hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t qs, const void* kc, const float* lse, float decay, float* w,
-                         int64_t ws, bool few, bool few_blocks, bool many, bool split, hipStream_t st) {
+                         int64_t ws, bool few, bool few_blocks, const PagedKeys* many, int n_many, bool split, hipStream_t st) {
   with_types(dtype, v.d, [&](auto dt, auto d) {
     constexpr int DT = decltype(dt)::value, D = decltype(d)::value;
     const int64_t qb = qs * element_bytes(DT);
@@ -1241,16 +1243,13 @@ hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t q
     const int keys = few_blocks ? 256 : 512;
     if (few) paged_weights_rows_kernel<DT, D><<<dim3((v.longest + keys - 1) / keys, v.n_kv, v.n_seq), 256, 0, st>>>(
         v, (const char*)q, qb, (const char*)kc, lse, decay, w, ws, keys);
-    if (many) {
-        auto launch = [&](auto split) {
-          constexpr bool SPLIT = decltype(split)::value;
-          constexpr int KEYS = SPLIT ? 32 : 128;
-          paged_weights_tile_kernel<DT, D, SPLIT><<<dim3((v.longest + KEYS - 1) / KEYS, v.n_kv, v.n_seq), 256, 0, st>>>(
-              v, (const char*)q, qb, (const char*)kc, lse, decay, w, ws);
-        };
-        if (split) launch(std::true_type{});
-        else launch(std::false_type{});
-      }
+    if (n_many > 0) {
+      if (split)
+        paged_weights_tile_kernel<DT, D, true><<<dim3(n_many * v.n_kv, kWeighKeys / 32), 256, 0, st>>>(
+            v, many, (const char*)q, qb, (const char*)kc, lse, decay, w, ws);
+      else
+        paged_weights_tile_kernel<DT, D, false><<<n_many * v.n_kv, 256, 0, st>>>(v, many, (const char*)q, qb, (const char*)kc, lse, decay, w, ws);
+    }
   });
   return hipGetLastError();
 }

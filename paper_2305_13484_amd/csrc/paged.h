@@ -47,6 +47,12 @@ struct PagedMerge {
   int row0, part, stride, parts, tile, pad[3];
 };
 
+// 128 positions of a sequence for the weights' tile kernel, those with the most rows of queries to go through first.
+struct PagedKeys {
+  int seq, key0;
+};
+constexpr int kWeighKeys = 128;
+
 struct PagedView {     // device memory of a plan, and the shape
   const PagedSeq* seqs;
   const int* pages;
@@ -63,10 +69,10 @@ hipError_t paged_append(int dtype, const PagedView& v, const void* k, int64_t ks
 // most_parts, most_rows: of any entry of merges
 hipError_t paged_attention(int dtype, const PagedView& v, const PagedItem* rows, int n_rows, const PagedItem* tiles, int n_tiles, const PagedMerge* merges, int n_merges,
                            int most_parts, int most_rows, const void* q, int64_t qs, const void* kc, const void* vc, void* out, float* lse, hipStream_t st);
-// few, many: whether there are sequences of the streaming kernel (those without new tokens among them), of the tile kernel; few_blocks, split:
+// few: whether there are sequences of the streaming kernel (those without new tokens among them); many: the tile kernel's work; few_blocks, split:
 // whether it has few blocks
 hipError_t paged_weights(int dtype, const PagedView& v, const void* q, int64_t qs, const void* kc, const float* lse, float decay, float* w,
-                         int64_t ws, bool few, bool few_blocks, bool many, bool split, hipStream_t st);
+                         int64_t ws, bool few, bool few_blocks, const PagedKeys* many, int n_many, bool split, hipStream_t st);
 hipError_t paged_evict(int dtype, const PagedView& v, void* kc, void* vc, const float* w, int64_t ws, int budget, int first, int recent,
                        float* wo, int64_t os, int* kept, hipStream_t st);
 

@@ -59,12 +59,12 @@ int check_shape(const flover_paged_shape* s) {
 // A plan's lists as they go to the device, and where each begins.
 struct Lists {
   std::vector<char> bytes;
-  size_t pages = 0, places = 0, rows = 0, tiles = 0, merges = 0;      // offsets; the sequences come first
+  size_t pages = 0, places = 0, rows = 0, tiles = 0, merges = 0, weigh = 0;      // offsets; the sequences come first
   size_t pm = 0, po = 0, total = 0;                        // partial results, behind the lists
-  int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_tiles = 0, n_merges = 0;
+  int n_seq = 0, tokens = 0, longest = 0, n_rows = 0, n_tiles = 0, n_merges = 0, n_weigh = 0;
   int most_parts = 0, most_rows = 0;                       // of a merge
-  bool few = false, many = false;                          // sequences of up to 16 rows per key head, of more,
-  int64_t row_blocks = 0, tile_blocks = 0;                 // and their blocks of 512, of 128 positions of a key head
+  bool few = false;                                        // sequences of up to 16 rows per key head,
+  int64_t row_blocks = 0;                                  // and their blocks of 512 positions of a key head
   bool shared = false, shared_new = false;                 // a page twice in use; one that new tokens go to
 };
 
@@ -106,6 +106,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   pages.reserve(n_pages);
   places.reserve(tokens);
   std::vector<uint8_t> used(sh.n_pages, 0);                // 1: read, 2: new tokens go there
+  std::vector<std::pair<int, flk::PagedKeys>> weigh;       // with the rows to go through
   int first = 0;
   for (int i = 0; i < n_seq; ++i) {
     const int need = (len[i] + sh.page_size - 1) / sh.page_size, fresh = len[i] - new_len[i];
@@ -114,8 +115,11 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
       L->few = true;
       L->row_blocks += ((int64_t)len[i] + 511) / 512 * sh.n_kv_head;
     } else {
-      L->many = true;
-      L->tile_blocks += ((int64_t)len[i] + 127) / 128 * sh.n_kv_head;
+      for (int k = 0; k < len[i]; k += flk::kWeighKeys) {       // tokens that see some of these positions
+        const int64_t end = (int64_t)std::min(len[i], k + flk::kWeighKeys) - 1 + sh.window - fresh;
+        const int64_t tokens_of = (sh.window > 0 && k >= sh.sinks ? std::min<int64_t>(new_len[i], end) : new_len[i]) - std::max(0, k - fresh);
+        weigh.push_back({(int)std::max<int64_t>(0, tokens_of) * group, {i, k}});
+      }
     }
     for (int p = 0; p < need; ++p) {
       const int page = table[(size_t)i * stride + p];
@@ -205,10 +209,15 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
       if (partial >= 2147483648LL) return bad("too many partial results");
     }
   }
-  if ((int64_t)std::max({rows.size(), tiles.size(), merges.size()}) * sh.n_kv_head >= 1 << 24) return bad("too much work for one launch");
+  if ((int64_t)std::max({rows.size(), tiles.size(), merges.size(), weigh.size()}) * sh.n_kv_head >= 1 << 24) return bad("too much work for one launch");
   L->n_rows = (int)rows.size();
   L->n_tiles = (int)tiles.size();
   L->n_merges = (int)merges.size();
+
+  std::stable_sort(weigh.begin(), weigh.end(), [](const auto& a, const auto& b) { return a.first > b.first; });
+  std::vector<flk::PagedKeys> weigh_keys(weigh.size());
+  for (size_t i = 0; i < weigh.size(); ++i) weigh_keys[i] = weigh[i].second;
+  L->n_weigh = (int)weigh_keys.size();
 
   size_t off = 0;
   auto put = [&](size_t bytes) {
@@ -222,6 +231,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   L->rows = put(rows.size() * sizeof(PagedItem));
   L->tiles = put(tiles.size() * sizeof(PagedItem));
   L->merges = put(merges.size() * sizeof(PagedMerge));
+  L->weigh = put(weigh_keys.size() * sizeof(flk::PagedKeys));
   L->bytes.assign(off, 0);
   auto fill = [&](size_t at, const void* from, size_t n) {
     if (n) std::memcpy(L->bytes.data() + at, from, n);
@@ -231,6 +241,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   fill(L->places, places.data(), places.size() * 4);
   fill(L->rows, rows.data(), rows.size() * sizeof(PagedItem));
   fill(L->tiles, tiles.data(), tiles.size() * sizeof(PagedItem));
+  fill(L->weigh, weigh_keys.data(), weigh_keys.size() * sizeof(flk::PagedKeys));
   fill(L->merges, merges.data(), merges.size() * sizeof(PagedMerge));
   L->pm = put((size_t)partial * 2 * 4);
   L->po = put((size_t)partial * sh.head_dim * 4);
@@ -469,7 +480,8 @@ int32_t flover_k_paged_weights(const flover_paged_plan* plan, const void* q, int
       return fail_call(FLOVER_E_INVAL, "the weights share memory with what is read");
     PAGED_TRY(ready(plan, (hipStream_t)stream));
     PAGED_HIP(flk::paged_weights(plan->shape.dtype, plan->view(), q, q_stride, kcache, lse, decay, weights, weight_stride, l.few,
-                                 l.row_blocks < 1024, l.many, l.tile_blocks <= 128, (hipStream_t)stream));
+                                 l.row_blocks < 1024, (const flk::PagedKeys*)(plan->memory + l.weigh), l.n_weigh,
+                                 (int64_t)l.n_weigh * plan->shape.n_kv_head <= 128, (hipStream_t)stream));
     return FLOVER_OK;
   });
 }
