@@ -71,9 +71,21 @@ __device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) 
 // permutation of a V row's 16-byte pieces (pairs stay together), so that the keys of a transposing read spread over the banks
 template <int D> __device__ __forceinline__ int piece_swizzle(int key) { return D == 128 ? (key & 7) * 2 : ((key >> 1) & 3) * 2; }
 
-template <int DT> __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
-  if constexpr (DT == DT_BF16) return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16);
-  else return (uint32_t)f32_to_f16(a) | ((uint32_t)f32_to_f16(b) << 16);
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+// Two values rounded to the 16-bit type, to nearest even, in a dword, and the values of its halves.
+template <int DT> __device__ __forceinline__ uint32_t round_pair(float a, float b) {      
+  if constexpr (DT == DT_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+  else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
+}
+template <int DT> __device__ __forceinline__ float low_half(uint32_t x) {
+  if constexpr (DT == DT_BF16) return __uint_as_float(x << 16);
+  else return f16_to_f32((uint16_t)(x & 0xffffu));
+}
+template <int DT> __device__ __forceinline__ float high_half(uint32_t x) {
+  if constexpr (DT == DT_BF16) return __uint_as_float(x & 0xffff0000u);
+  else return f16_to_f32((uint16_t)(x >> 16));
 }
 
 // Four V^T operands (8 keys of 16 d each) by transposing reads; a[i]: this lane's LDS address of operand i, the second 16 keys lie HI
@@ -227,12 +239,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
         for (int dt = 0; dt < DTL; ++dt)
           oacc[dt] = mfma_f32(*(const float*)(mv + (4 * g + r) * RB + ((dt * 4 + (n >> 2)) ^ (g * 4)) * 16 + (n & 3) * 4), p[r], oacc[dt]);
     } else {
-      float rest[8];
+      u32x4_t hi, lo;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) rest[j] = p[j] - rdt<DT>(p[j]);
-      const u32x4_t hi = {pack_pair<DT>(p[0], p[1]), pack_pair<DT>(p[2], p[3]), pack_pair<DT>(p[4], p[5]), pack_pair<DT>(p[6], p[7])};
-      const u32x4_t lo = {pack_pair<DT>(rest[0], rest[1]), pack_pair<DT>(rest[2], rest[3]), pack_pair<DT>(rest[4], rest[5]),
-                          pack_pair<DT>(rest[6], rest[7])};
+      for (int j = 0; j < 4; ++j) {
+        hi[j] = round_pair<DT>(p[2 * j], p[2 * j + 1]);
+        lo[j] = round_pair<DT>(p[2 * j] - low_half<DT>(hi[j]), p[2 * j + 1] - high_half<DT>(hi[j]));
+      }
 #pragma unroll
       for (int d4 = 0; d4 < DTL; d4 += 4) {
         uint32_t at[4];
@@ -334,9 +346,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 // ---------------------------------------------------------------- attention, many rows per key head
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
-typedef __attribute__((ext_vector_type(2))) float f32x2_t;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
 
 // D[32][32] += A[32][16] . B[16][32]: a lane holds row (column) lane % 32 of A (B), 8 consecutive k from 8 * (lane / 32), and of D column lane % 32,
 // rows i % 4 + 8 * (i / 4) + 4 * (lane / 32), i < 16
@@ -345,10 +354,6 @@ template <int DT> __device__ __forceinline__ f32x16_t mfma32(const u32x4_t& a, c
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-}
-template <int DT> __device__ __forceinline__ uint32_t round_pair(float a, float b) {      // to nearest even
-  if constexpr (DT == DT_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
-  else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
 }
 // V^T operands of twice 16 keys (RB * 16 bytes apart, OFF bytes from a on) and N times 32 d by transposing reads: 16 lanes give the addresses of 4 keys
 // x 16 d and get 4 keys of one d each; the second four keys of a lane lie 8 rows further.  The wait stands in the block.
