@@ -34,7 +34,7 @@ __device__ __forceinline__ uint32_t cache_row(const PagedView& v, const PagedSeq
 
 // ---------------------------------------------------------------- rows of new tokens
 
-// A thread moves 16 bytes of one key head's row of K or V (blockIdx.y).
+// A thread moves 16 bytes of one key head's row of K or V (blockIdx.y); memory bounds it (47 MB read and written in 8.9 us).
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedView v, const char* __restrict__ k, int64_t ks, const char* __restrict__ vv,
                                                            int64_t vs, char* __restrict__ kc, char* __restrict__ vc, int row_pieces) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -75,7 +75,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
 // Two values rounded to the 16-bit type, to nearest even, in a dword, and the values of its halves.
-template <int DT> __device__ __forceinline__ uint32_t round_pair(float a, float b) {      
+template <int DT> __device__ __forceinline__ uint32_t round_pair(float a, float b) {
   if constexpr (DT == DT_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
   else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
 }
@@ -115,14 +115,16 @@ template <int HI> __device__ __forceinline__ void read_keys_of_d(const uint32_t 
 //            leaves the time for it.
 // Keys that a row does not see have weight zero; if the sum comes out infinite or as no number all the same, it may be such a key's V (0 x inf),
 // and the wave's steps are gone through again with those elements kept out of the product and added where they are seen.
+// Whole rows go to registers and from there to the wave's LDS, K as well: loading operands straight (16 rows x 64 bytes an instruction, 300 registers,
+// one wave per SIMD) read 1.07 GB (64 requests of up to 8192 rows, 32 heads on 8, bf16) in 259 us; this way, two waves per SIMD, in 176 (6.1 TB/s).
 template <int DT, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_rows_kernel(PagedView v, const PagedItem* __restrict__ items, const char* __restrict__ q,
-                                                         int64_t qs, const char* __restrict__ kc, const char* __restrict__ vc,
-                                                         void* __restrict__ out, float* __restrict__ lse) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_rows_kernel(
+    PagedView v, const PagedItem* __restrict__ items, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc,
+    const char* __restrict__ vc, void* __restrict__ out, float* __restrict__ lse) {
   constexpr int EB = DT == DT_F32 ? 4 : 2, RB = D * EB;       // bytes of an element, of a row
   constexpr int KT = DT == DT_F32 ? 16 : 32, KG = KT / 16;
   constexpr int KS = RB / 64;               // 64-byte steps over a row
-  constexpr int LPR = RB / 16, RPI = 64 / LPR, NV = KT / RPI;  // V: lanes per row, rows per load, loads of a step
+  constexpr int LPR = RB / 16, RPI = 64 / LPR, NV = KT / RPI;  // lanes per row, rows per load, loads of a step of K, of V
   constexpr int DTL = D / 16;
   constexpr int LD = D + 4;                 // floats per row of the merge
   constexpr int STEP = KT * RB;             // bytes of a step of K, of V
@@ -416,6 +418,10 @@ template <int OFF> __device__ __forceinline__ void read_pieces(const uint32_t (&
 //            output's own rounding; the sum in the denominator is of the unrounded ones); V^T by transposing reads.
 // LDS rows are the cache's, their 16-byte pieces permuted by key so that a read's keys spread over the banks.  Steps that every row of the wave
 // sees in full take no mask.  A sum that is infinite or no number: as in paged_rows_kernel, the block goes through its keys again.
+// Per step and wave the matrix unit has 1024 cycles (d = 128), the vector unit about 900 (32 exponentials of 16 cycles each, and the maximum, the
+// scaling, the sum, the rounding of 32 scores), the compute unit's LDS 256; two waves of different blocks share a SIMD, and one that has its scores
+// goes first.  2 x 2048 tokens over 7000 and 8192 rows, 32 heads on 8, bf16: 436 us, 1.01 PFLOP/s (without that priority 456; with LDS reads that
+// the compiler waits for copies at 567; 16 rows per block 3680).
 template <int DT, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_tile_kernel(
     PagedView v, const PagedItem* __restrict__ items, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc,
@@ -686,7 +692,7 @@ __device__ __forceinline__ float new_weight(float given, float old, float decay,
 
 // grid = (blocks of `keys` positions, n_kv, n_seq).  Few rows of queries: K streams through as in paged_rows_kernel (a wave takes every
 // fourth step, whole rows to registers, to the wave's piece of LDS, from there as operands) and bounds it.  S[row][key] = Q . K^T leaves a key's
-// scores in one column, so that their exponentials add up in a lane.
+// scores in one column, so that their exponentials add up in a lane.  64 requests of 4096 rows, 8 key heads, bf16: 92 us (5.8 TB/s).
 template <int DT, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F32 ? 2 : 4))) void paged_weights_rows_kernel(PagedView v, const char* __restrict__ q, int64_t qs,
                                                                  const char* __restrict__ kc, const float* __restrict__ lse, float decay,
@@ -793,7 +799,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F3
 // 1000 rows 6.2 -> 5.0, 32 heads on 8, 1000 of 1000 64 -> 27; 128 blocks, 200 of 2000 18.8 -> 12.4, 2000 of 2000 122 -> 90; 192 blocks, 16 heads,
 // 1500 of 1500 28.1 -> 24.2, 500 of 1500 13.4 -> 16.2; 256 blocks, 32 heads, 1000 of 1000 20.9 -> 26.9).
 // 16-bit types: vector instructions bound it, an exponential takes 16 cycles of a wave, its product's share 8, the sum and the scaling 4 each.  fp32:
-// the products (16 x 16 x 4).
+// the products (16 x 16 x 4).  2048 new tokens of 8192 rows, 32 heads on 8, bf16: 180 us; 1000 of 3000, fp32: 315.
 
 // The rows of a block's, or of a wave's, steps and their lse.
 template <int RB, int ROWS, int WAVES, int RING> struct QueryRing {
@@ -1023,7 +1029,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 // A block per (key head, sequence).  The weight of the last row kept is found digit by digit from the top (four digits of 8 bits, counted
 // in LDS); rows of exactly that weight are taken from the front.  Then the positions are gone through in order, four per thread, and numbered.  The
-// weights' keys stay in LDS (the first kKeysHeld of them; of a longer sequence the rest is read again).
+// weights' keys stay in LDS (the first kKeysHeld of them; of a longer sequence the rest is read again).  32 sequences of up to 4096 rows, 8 key heads:
+// 9.8 us, a chain of dependent steps.
 constexpr int kKeysHeld = 18432;           // 72 KB: two blocks per compute unit
 // Sums over the lanes up to and including one's own, of the wave; lanes without a source add zero.
 template <int CTRL, int ROWS> __device__ __forceinline__ int plus_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
@@ -1139,7 +1146,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const f
 // at a time.
 // A row moves to a place at or in front of its own, and a place is overwritten only once every row up to it has been read: a
 // barrier between the reads (waited for) and the writes of a batch is enough, because the batch behind reads from places behind.  Where the rows of
-// the next batch lie and go is looked up, a row per thread, while a batch is read.
+// the next batch lie and go is looked up, a row per thread, while a batch is read.  28 sequences to 1024 rows of 8 x 256 bytes, K and V: 52 us.
 // 128 bytes of a row where there are blocks enough, otherwise 32: four times the blocks, and a quarter of the batches one after the other.
 constexpr int kMove = 8;
 template <int PIECES>

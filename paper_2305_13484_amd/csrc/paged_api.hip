@@ -68,9 +68,15 @@ struct Lists {
   bool shared = false, shared_new = false;                 // a page twice in use; one that new tokens go to
 };
 
-// Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long: two of either are at work
-// on a compute unit.
+// Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long: two of either are at work on a
+// compute unit, 512 in all.  The streaming kernel's take between the two figures, 32 steps each where there are so many (us at 512 / 1024 / 2048 / 3072
+// blocks, single tokens, bf16, d = 128: 64 sequences of up to 8192 rows on 8 key heads, 65536 steps, 214 / 192 / 186 / 185; 4 of 20000 to 30000, 25000
+// steps, 78 / 78 / 85 / 90; 32 of up to 1000, 32 key heads, 56 / 55 / 58 / 60).  The tile kernel leaves partial results of 66 KB per block: 512 new tokens
+// of 4096 rows, 32 heads on 8, at 256 / 512 / 768 / 1024 blocks 62 / 56 / 69 / 70; 2 x 2048 of 8192 453 / 445 / 443 / 442.
 constexpr int kBlocks[2][2] = {{1024, 2048}, {512, 512}};
+// No parts at all where no row has more steps than this: the launch that joins them costs about 3 us of the host's time and of the GPU's (whole ->
+// parts, us: a tiny fp32 model's 7 requests of up to 128 rows 9.2 -> 11.7 a call; on the GPU 16 sequences of up to 300, 16 key heads, 10.6 -> 13.8, 64 of
+// up to 300, 8 key heads, 16.7 -> 21.9, one of 400 9.0 -> 7.1, of 700 14.7 -> 8.0; tiles, 2 x 300 tokens 14.2 -> 17.2, 64 tokens of 1000 rows 27.2 -> 15.8).
 constexpr int kWhole[2] = {16, 8};
 
 int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const int32_t* len, const int32_t* table, int stride, Lists* L) {
