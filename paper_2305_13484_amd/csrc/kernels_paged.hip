@@ -420,7 +420,7 @@ template <int OFF> __device__ __forceinline__ void read_pieces(const uint32_t (&
 // sees in full take no mask.  A sum that is infinite or no number: as in paged_rows_kernel, the block goes through its keys again.
 // Per step and wave the matrix unit has 1024 cycles (d = 128), the vector unit about 900 (32 exponentials of 16 cycles each, and the maximum, the
 // scaling, the sum, the rounding of 32 scores), the compute unit's LDS 256; two waves of different blocks share a SIMD, and one that has its scores
-// goes first.  2 x 2048 tokens over 7000 and 8192 rows, 32 heads on 8, bf16: 436 us, 1.01 PFLOP/s (without that priority 456; with LDS reads that
+// goes first.  2 x 2048 tokens over 7000 and 8192 rows, 32 heads on 8, bf16: 420 to 436 us, 1.01 to 1.05 PFLOP/s (without that priority 3 % more; with LDS reads that
 // the compiler waits for copies at 567; 16 rows per block 3680).
 template <int DT, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_tile_kernel(
@@ -1146,7 +1146,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedView v, const f
 // at a time.
 // A row moves to a place at or in front of its own, and a place is overwritten only once every row up to it has been read: a
 // barrier between the reads (waited for) and the writes of a batch is enough, because the batch behind reads from places behind.  Where the rows of
-// the next batch lie and go is looked up, a row per thread, while a batch is read.  28 sequences to 1024 rows of 8 x 256 bytes, K and V: 52 us.
+// the next batch lie and go is looked up, a row per thread, while a batch is read.  28 sequences to 1024 rows of 8 x 256 bytes, K and V: 45 to 52 us.
 // 128 bytes of a row where there are blocks enough, otherwise 32: four times the blocks, and a quarter of the batches one after the other.
 constexpr int kMove = 8;
 template <int PIECES>
