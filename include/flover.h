@@ -384,8 +384,8 @@ int32_t flover_k_paged_plan_set(flover_paged_plan* plan, int32_t n_seq, const in
 int32_t flover_k_paged_plan_destroy(flover_paged_plan* plan);   /* waits for the plan's last copy; NULL is a no-op */
 
 /* Rows of the new tokens to their places: k, v [device][T] rows of [n_kv_head][head_dim], k_stride / v_stride elements apart
- * (a multiple of 16 bytes, at most 16 MB; views into a packed q|k|v row are fine), 16-byte aligned.  Refused (INVAL) where two sequences of
- * the plan share a page that new tokens go to. */
+ * (a multiple of 16 bytes, at most 16 MB; views into a packed q|k|v row are fine), 16-byte aligned.  Refused (INVAL)
+ * where a page that new tokens go to stands twice in the plan's lists. */
 int32_t flover_k_paged_append(const flover_paged_plan* plan, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                               void* kcache, void* vcache, void* stream);
 
@@ -413,7 +413,7 @@ int32_t flover_k_paged_weights(const flover_paged_plan* plan, const void* q, int
  * plan has min(len, budget) rows for the sequence, and its further pages are free.
  * weights: as above.  weights_out [device][n_seq][n_kv_head] rows of out_stride >= min(budget, longest): the kept rows' weights (the rest
  * stays); may be `weights` itself with the same stride, otherwise apart from it; NULL: not wanted.  kept [device][n_seq][n_kv_head][budget]:
- * the positions that were kept, -1 behind the last.  Refused (INVAL) where sequences of the plan share a page, and where
+ * the positions that were kept, -1 behind the last.  Refused (INVAL) where a page stands twice in the plan's lists, and where
  * first + recent > budget. */
 int32_t flover_k_paged_evict(const flover_paged_plan* plan, void* kcache, void* vcache, const float* weights, int64_t weight_stride,
                              int32_t budget, int32_t first, int32_t recent, float* weights_out, int64_t out_stride, int32_t* kept,

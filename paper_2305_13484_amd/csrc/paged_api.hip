@@ -430,7 +430,7 @@ int32_t flover_k_paged_append(const flover_paged_plan* plan, const void* k, int6
     if (overlap(kcache, nc, vcache, nc) || overlap(kcache, nc, k, nk) || overlap(kcache, nc, v, nv) || overlap(vcache, nc, k, nk) ||
         overlap(vcache, nc, v, nv))
       return fail_call(FLOVER_E_INVAL, "the caches share memory with each other or with the rows");
-    if (plan->lists.shared_new) return fail_call(FLOVER_E_INVAL, "new tokens go to a page that another sequence has too");
+    if (plan->lists.shared_new) return fail_call(FLOVER_E_INVAL, "new tokens go to a page that is in use elsewhere, by another sequence or the same");
     PAGED_TRY(ready(plan, (hipStream_t)stream));
     PAGED_HIP(flk::paged_append(plan->shape.dtype, plan->view(), k, k_stride, v, v_stride, kcache, vcache, (hipStream_t)stream));
     return FLOVER_OK;

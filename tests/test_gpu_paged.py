@@ -60,6 +60,50 @@ def test_attention_in_a_window(fl, dtype, d, window, sinks):
     check_attention(fl, Case(dtype, 8, 4, d, 32, new, lens, window, sinks, seed=window))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n_head,n_kv,d", [(40, 1, 128), (64, 1, 64), (34, 2, 64)])
+def test_many_heads_on_one_key_head(fl, dtype, n_head, n_kv, d):
+    """More than 16 rows from a single token; groups that do not divide a tile."""
+    c = Case(dtype, n_head, n_kv, d, 16, [1, 1, 1, 7], [1, 40, 700, 130], seed=d)
+    check_attention(fl, c)
+    check_weights(fl, c, 0.5)
+    check_attention(fl, Case(dtype, n_head, n_kv, d, 16, [1, 5], [300, 77], 50, 3, seed=d))
+
+
+@pytest.mark.parametrize("page,lens", [(1, [1, 1, 0]), (7, [7, 3]), (16, [16])])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_the_smallest_pages(fl, dtype, page, lens):
+    for new in ([min(n, 1) for n in lens], lens):
+        c = Case(dtype, 4, 2, 64, page, new, lens, seed=page)
+        check_attention(fl, c)
+        check_weights(fl, c, 1.0)
+
+
+def test_nothing_new_ages_the_weights_alone(fl):
+    c = Case(BF, 4, 2, 64, 16, [0, 0], [40, 17], seed=1)
+    w = torch.rand(2, 2, 50, device="cuda")
+    ref = w.clone()
+    ref[0, :, :40] *= 0.5
+    ref[1, :, :17] *= 0.5
+    none = torch.zeros(0, 4, 64, dtype=BF, device="cuda")
+    plan = c.plan(fl)
+    assert torch.equal(fl.k_paged_weights(plan, none, c.k.cuda(), torch.zeros(0, 4, device="cuda"), w, decay=0.5), ref)
+    assert fl.k_paged_attention(plan, none, c.k.cuda(), c.v.cuda()).shape == (0, 4, 64)
+
+
+def test_a_page_twice_in_one_sequence(fl):
+    """Read, it is the same rows twice; writing to it is refused."""
+    c = Case(BF, 4, 2, 64, 16, [1], [64], seed=1)
+    c.table[0][2] = c.table[0][1]
+    check_attention(fl, c)
+    with pytest.raises(fl.FloverError, match="in use twice"):
+        fl.k_paged_evict(c.plan(fl), c.k.cuda(), c.v.cuda(), torch.rand(1, 2, 64, device="cuda"), 30)
+    c.table[0][3] = c.table[0][0]
+    k = torch.randn(1, 2, 64, device="cuda").to(BF)
+    with pytest.raises(fl.FloverError, match="another sequence"):
+        fl.k_paged_append(c.plan(fl), k, k, c.k.cuda(), c.v.cuda())
+
+
 def test_a_window_longer_than_any_sequence_is_none(fl):
     c = Case(BF, 8, 2, 64, 16, [1, 40], [300, 90], seed=2)
     q, k, v, lse = c.q.cuda(), c.k.cuda(), c.v.cuda(), c.attention()[1].float().cuda()
