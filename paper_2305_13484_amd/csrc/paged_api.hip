@@ -69,15 +69,18 @@ struct Lists {
 };
 
 // Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long: two of either are at work on a
-// compute unit, 512 in all.  The streaming kernel's take between the two figures, 32 steps each where there are so many (us at 512 / 1024 / 2048 / 3072
-// blocks, single tokens, bf16, d = 128: 64 sequences of up to 8192 rows on 8 key heads, 65536 steps, 214 / 192 / 186 / 185; 4 of 20000 to 30000, 25000
+// compute unit, 512 in all.  Between the two figures kShare steps each, where there are so many (us at 512 / 1024 / 2048 / 3072 blocks of the streaming
+// kernel, single tokens, bf16, d = 128: 64 sequences of up to 8192 rows on 8 key heads, 65536 steps, 214 / 192 / 186 / 185; 4 of 20000 to 30000, 25000
 // steps, 78 / 78 / 85 / 90; 32 of up to 1000, 32 key heads, 56 / 55 / 58 / 60).  The tile kernel leaves partial results of 66 KB per block: 512 new tokens
-// of 4096 rows, 32 heads on 8, at 256 / 512 / 768 / 1024 blocks 62 / 56 / 69 / 70; 2 x 2048 of 8192 453 / 445 / 443 / 442.
-constexpr int kBlocks[2][2] = {{1024, 2048}, {512, 512}};
-// No parts at all where no row has more steps than this: the launch that joins them costs about 3 us of the host's time and of the GPU's (whole ->
-// parts, us: a tiny fp32 model's 7 requests of up to 128 rows 9.2 -> 11.7 a call; on the GPU 16 sequences of up to 300, 16 key heads, 10.6 -> 13.8, 64 of
-// up to 300, 8 key heads, 16.7 -> 21.9, one of 400 9.0 -> 7.1, of 700 14.7 -> 8.0; tiles, 2 x 300 tokens 14.2 -> 17.2, 64 tokens of 1000 rows 27.2 -> 15.8).
-constexpr int kWhole[2] = {16, 8};
+// of 4096 rows, 32 heads on 8, 7800 steps, at 256 / 512 / 768 / 1024 blocks 62 / 56 / 69 / 70; 2 x 2048 of 8192 453 / 445 / 443 / 442; at 512 / 256 3 x 187
+// of up to 3132, 5 heads, 24.5 / 22.3.
+constexpr int kBlocks[2][2] = {{1024, 2048}, {256, 512}}, kShare[2] = {32, 8};
+// No parts at all where no row has more steps than this, in launches of up to 64 blocks and of more: the launch that joins them costs about 3 us of the
+// host's time and of the GPU's, a step of a wave 1.7 (four steps of the streaming kernel's rows), of the tile kernel 1.15.  Whole -> parts, us:
+// a tiny fp32 model's 7 requests of up to 128 rows 9.2 -> 11.7 a call; on the GPU 16 sequences of up to 300, 16 key heads, 10.6 -> 13.8, 64 of up to 300, 8 key
+// heads, 16.7 -> 21.9, one of 400 9.0 -> 7.1, of 700 14.7 -> 8.0; tiles, 16 tokens of 512 rows, 8 blocks, 15.9 -> 10.2, 3 x 161 to 322 tokens, 112 blocks, 16.2 ->
+// 19.2.
+constexpr int kWhole[2][2] = {{16, 16}, {4, 8}};
 
 int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const int32_t* len, const int32_t* table, int stride, Lists* L) {
   auto bad = [](const std::string& m) { return fail_call(FLOVER_E_INVAL, m); };
@@ -173,11 +176,12 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
       }
     }
     std::stable_sort(items.begin(), items.end(), [](const PagedItem& a, const PagedItem& b) { return a.u1 > b.u1; });
-    // The least share of steps, four at least, that makes no more blocks than `most`
+    // The least share of steps that makes no more blocks than `most`, a step per wave of the streaming kernel, two of the tile kernel at least
     const int64_t all = steps * sh.n_kv_head;
-    const int64_t most = std::min<int64_t>(kBlocks[kind][1], std::max<int64_t>(kBlocks[kind][0], all / 32));
-    // ... and none at all where no row has more than kWhole steps: the launch that joins parts costs more than they save
-    int64_t share = std::max<int64_t>(longest <= kWhole[kind] ? longest : 4, (all + most - 1) / most);
+    const int64_t most = std::min<int64_t>(kBlocks[kind][1], std::max<int64_t>(kBlocks[kind][0], all / kShare[kind]));
+    // ... and none at all where no row has more than kWhole steps
+    const int whole = (int64_t)items.size() * sh.n_kv_head <= 64 ? kWhole[kind][0] : kWhole[kind][1];
+    int64_t share = std::max<int64_t>(longest <= whole ? longest : kind ? 2 : 4, (all + most - 1) / most);
     for (int64_t low = share, high = std::max<int64_t>(share, longest); low < high; share = high) {
       const int64_t mid = (low + high) / 2;
       int64_t blocks = 0;
