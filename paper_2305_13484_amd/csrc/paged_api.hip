@@ -69,9 +69,9 @@ struct Lists {
 };
 
 // Blocks that a launch of the streaming kernel, of the tile kernel, is cut into where sequences are few and long: two of either are at work on a
-// compute unit, 512 in all.  Between the two figures kShare steps each, where there are so many (us at 512 / 1024 / 2048 / 3072 blocks of the streaming
-// kernel, single tokens, bf16, d = 128: 64 sequences of up to 8192 rows on 8 key heads, 65536 steps, 214 / 192 / 186 / 185; 4 of 20000 to 30000, 25000
-// steps, 78 / 78 / 85 / 90; 32 of up to 1000, 32 key heads, 56 / 55 / 58 / 60).  The tile kernel leaves partial results of 66 KB per block: 512 new tokens
+// compute unit, 512 in all.  Between the two figures kShare steps each, where there are so many (us at 512 / 1024 / 2048 blocks of the streaming
+// kernel, single tokens, bf16, d = 128: 64 sequences of up to 8192 rows on 8 key heads, 65536 steps, 214 / 192 / 186; 4 of 20000 to 30000, 25000
+// steps, 78 / 78 / 85; 32 of up to 1000, 32 key heads, 56 / 55 / 58).  The tile kernel leaves partial results of 66 KB per block: 512 new tokens
 // of 4096 rows, 32 heads on 8, 7800 steps, at 256 / 512 / 768 / 1024 blocks 62 / 56 / 69 / 70; 2 x 2048 of 8192 453 / 445 / 443 / 442; at 512 / 256 3 x 187
 // of up to 3132, 5 heads, 24.5 / 22.3.
 constexpr int kBlocks[2][2] = {{1024, 2048}, {256, 512}}, kShare[2] = {32, 8};
