@@ -349,7 +349,8 @@ int32_t flover_k_gated_mlp(int32_t dtype, const void* x, const void* w_tiled, in
  * lie in pages, attention may be bounded by a window, and a cache may be cut down to its heaviest rows.
  * One layer's cache is kcache, vcache [device][n_pages][n_kv_head][page_size][head_dim]; position p of a sequence lies in row
  * p % page_size of page table[p / page_size].  A slot cache [C][n_head][S][head_dim] is the case page_size = S with one page
- * per sequence.  Query head h reads key head h / (n_head / n_kv_head). */
+ * per sequence.  Query head h reads key head h / (n_head / n_kv_head).
+ * The calls enqueue on `stream`, whose device is the current one, and return without waiting. */
 typedef struct flover_paged_shape {
   int32_t dtype;                         /* FLOVER_F32 | FLOVER_F16 | FLOVER_BF16: queries, cache, output */
   int32_t n_head, n_kv_head, head_dim;   /* n_head a multiple of n_kv_head; head_dim in {64,128} */

@@ -697,9 +697,9 @@ __device__ __forceinline__ float new_weight(float given, float old, float decay,
 // fourth step, whole rows to registers, to the wave's piece of LDS, from there as operands) and bounds it.  S[row][key] = Q . K^T leaves a key's
 // scores in one column, so that their exponentials add up in a lane.  64 requests of 4096 rows, 8 key heads, bf16: 92 us (5.8 TB/s).
 template <int DT, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F32 ? 2 : 4))) void paged_weights_rows_kernel(PagedView v, const char* __restrict__ q, int64_t qs,
-                                                                 const char* __restrict__ kc, const float* __restrict__ lse, float decay,
-                                                                 float* __restrict__ w, int64_t ws, int keys) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DT == DT_F32 ? 2 : 4))) void paged_weights_rows_kernel(
+    PagedView v, const char* __restrict__ q, int64_t qs, const char* __restrict__ kc, const float* __restrict__ lse, float decay,
+    float* __restrict__ w, int64_t ws, int keys) {
   constexpr int EB = DT == DT_F32 ? 4 : 2, RB = D * EB, KS = RB / 64;
   constexpr int KT = DT == DT_F32 ? 16 : 32, KG = KT / 16, LPR = RB / 16, RPI = 64 / LPR, NV = KT / RPI;
   __shared__ __attribute__((aligned(1024))) char lds[4][KT * RB];

@@ -106,6 +106,7 @@ int build(const flover_paged_shape& sh, int n_seq, const int32_t* new_len, const
   // what the kernels count in 32 bits: rows of queries, and the threads of a launch
   if (tokens * sh.n_head >= 2147483648LL || tokens * sh.n_kv_head * (sh.head_dim * esize(sh.dtype) / 16) >= 4294967296LL)
     return bad("too many new tokens");
+  if (n_pages >= 2147483648ULL) return bad("too many pages");
   L->n_seq = n_seq;
   L->tokens = (int)tokens;
 
@@ -464,8 +465,8 @@ int32_t flover_k_paged_attention(const flover_paged_plan* plan, const void* q, i
     PAGED_TRY(ready(plan, (hipStream_t)stream));
     const Lists& l = plan->lists;
     PAGED_HIP(flk::paged_attention(plan->shape.dtype, plan->view(), (const PagedItem*)(plan->memory + l.rows), l.n_rows,
-                                   (const PagedItem*)(plan->memory + l.tiles), l.n_tiles, (const PagedMerge*)(plan->memory + l.merges), l.n_merges, l.most_parts, l.most_rows, q, q_stride, kcache, vcache, out, lse,
-                                   (hipStream_t)stream));
+                                   (const PagedItem*)(plan->memory + l.tiles), l.n_tiles, (const PagedMerge*)(plan->memory + l.merges),
+                                   l.n_merges, l.most_parts, l.most_rows, q, q_stride, kcache, vcache, out, lse, (hipStream_t)stream));
     return FLOVER_OK;
   });
 }
