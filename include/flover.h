@@ -374,7 +374,8 @@ typedef struct flover_paged_shape {
  * the plan on another stream wait for that copy by themselves (not while they are captured into a graph: then the copy has to
  * be done).  set cannot be captured (STATE).
  * Calls that use one plan share its memory: they may not overlap each other; plans in memory of their own may.
- * A captured call keeps the plan's launch shapes; it may be replayed until the plan is set again or destroyed.
+ * A captured call keeps the plan's launch shapes; it may be replayed, on a stream that is behind the copy, until the plan is set
+ * again or destroyed.
  * Errors: INVAL (shape, lengths, a page out of range, alignment), NOMEM, STATE, HIP. */
 typedef struct flover_paged_plan flover_paged_plan;
 int32_t flover_k_paged_plan_bytes(const flover_paged_shape* shape, int32_t n_seq, const int32_t* new_len, const int32_t* len,
